@@ -112,6 +112,61 @@ int sdden_mlp_select_gemm(sdden* den, int32_t variant);
 int sdden_destroy(sdden* den);
 const char* sdden_last_error(const sdden* den);
 
+/* ---- Layers of row networks ------------------------------------------------------------------------------------------
+ * What a denoiser of pre-norm residual blocks, h <- h + FF(LN(h)), is made of, forward for evaluating it and backward for
+ * fitting it (or a draft model of it).  Plain calls without a handle: every buffer is the caller's device memory, kernels are
+ * enqueued on `stream` only, nothing is allocated, synchronised or kept between calls, so any number may run at once on buffers
+ * of their own, and all of them may be captured into a graph.  Matrices are row-major; a `*_stride` is the number of elements
+ * between two rows.  Buffers must not overlap.  Errors: SD_ERR_* with the text in sdden_last_error(NULL), which is kept per
+ * thread; nothing is enqueued then.  R = 0 is no error: no row is written, weight gradients become zero. */
+#define SDDEN_F32 0
+#define SDDEN_BF16 1
+#define SDDEN_SILU 0              /* f(g) = g / (1 + exp(-g))                                     */
+#define SDDEN_GELU 1              /* f(g) = g P(g), P the normal distribution function            */
+
+/* Layer norm:  y = (x - mean) rstd * weight + bias,  rstd = 1 / sqrt(mean((x - mean)^2) + eps), statistics in fp32.
+ * x [R,d] of x_type, y [R,d] of y_type (any mix), weight and bias [d] fp32 or NULL (1 and 0), mean and rstd [R] fp32: both
+ * written for the backward pass, or both NULL.  Any d > 0, any stride >= d, any alignment of the element type; 16-byte
+ * accesses are used where d, the strides and the pointers allow them. */
+int sdden_layernorm_forward(int32_t R, int32_t d, const void* x, int32_t x_type, int64_t x_stride, const float* weight,
+                            const float* bias, float eps, void* y, int32_t y_type, int64_t y_stride, float* mean, float* rstd,
+                            void* stream);
+
+/* Its backward pass from dy [R,d] of dy_type and the forward pass's x, mean and rstd:
+ *   dx = rstd (g - mean(g) - xh mean(g xh)) + dres,  g = dy * weight,  xh = (x - mean) rstd      (x_type)
+ *   dweight = sum over rows dy xh,  dbias = sum over rows dy                                      (fp32 [d], each may be NULL)
+ * dres [R,d] of x_type: a gradient added to dx (the one that reaches x around the block, on the residual path), or NULL.
+ * workspace: sdden_layernorm_workspace_bytes(R, d) bytes where dweight or dbias is asked for, else NULL is enough.  Sums over rows
+ * are taken in a fixed order: the same call gives the same bits. */
+size_t sdden_layernorm_workspace_bytes(int32_t R, int32_t d);
+int sdden_layernorm_backward(int32_t R, int32_t d, const void* dy, int32_t dy_type, int64_t dy_stride, const void* x, int32_t x_type,
+                             int64_t x_stride, const float* weight, const float* mean, const float* rstd, const void* dres,
+                             int64_t dres_stride, void* dx, int64_t dx_stride, float* dweight, float* dbias, void* workspace,
+                             size_t workspace_bytes, void* stream);
+
+/* Gated feed-forward block:  hidden = f(X Wg^T) * (X Wu^T),  Y = hidden Wd^T + res.
+ * X [R,d], Wg and Wu [H,d], Wd [d,H], hidden [R,H]: bf16 bit patterns, the weights contiguous with one row per OUTPUT feature
+ * (sdden_mlp_create takes its weights the other way round).  Y and res [R,d] of y_type with the same stride; res may be NULL.
+ * hidden is scratch of an evaluation and an input of the backward pass; it is the one intermediate that is rounded to bf16,
+ * as the second product takes it.  gates [2,R,H] fp32: g = X Wg^T and u = X Wu^T for the backward pass (kept in fp32, so that
+ * gradients see no second rounding), or NULL.  d, H and the strides are multiples of 8 (16 bytes) up to 2^23; buffers are 16-byte
+ * aligned. */
+int sdden_gated_forward(int32_t R, int32_t d, int32_t H, int32_t act, const uint16_t* X, int64_t x_stride, const uint16_t* Wg,
+                        const uint16_t* Wu, const uint16_t* Wd, const void* res, void* Y, int32_t y_type, int64_t y_stride,
+                        uint16_t* hidden, float* gates, void* stream);
+
+/* Its backward pass from dY [R,d] (bf16) and the forward pass's X, gates and hidden.  With dA = dY Wd, dG = dA u f'(g) and
+ * dU = dA f(g), the last two rounded to bf16 for the products that take them:
+ *   dX = dG Wg + dU Wu  (bf16 [R,d], or NULL);  dWg = dG^T X, dWu = dU^T X [H,d], dWd = dY^T hidden [d,H], of dw_type (all
+ *   three, or all NULL).
+ * The gradient of res is dY itself.  workspace: sdden_gated_workspace_bytes(R, d, H) bytes, 16-byte aligned. */
+size_t sdden_gated_workspace_bytes(int32_t R, int32_t d, int32_t H);
+int sdden_gated_backward(int32_t R, int32_t d, int32_t H, int32_t act, const uint16_t* dY, int64_t dy_stride, const uint16_t* X,
+                         int64_t x_stride, const uint16_t* Wg, const uint16_t* Wu, const uint16_t* Wd, const float* gates,
+                         const uint16_t* hidden, uint16_t* dX, int64_t dx_stride, void* dWg, void* dWu, void* dWd,
+                         int32_t dw_type, void* workspace, size_t workspace_bytes, void* stream);
+
+
 #ifdef __cplusplus
 }
 #endif

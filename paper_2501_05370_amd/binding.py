@@ -26,6 +26,10 @@ SD_STATIC_MAX_CHAINS = 65536
 SD_CARRY_DRAFT = 0
 SD_CARRY_LAST_ACCEPTED = 1
 SD_ERR_UNSUPPORTED = -5
+SDDEN_F32 = 0
+SDDEN_BF16 = 1
+SDDEN_SILU = 0
+SDDEN_GELU = 1
 
 
 class SDError(RuntimeError):
@@ -90,6 +94,16 @@ _SIGNATURES = {
     "sdden_mlp_select_gemm": (c_int, [c_void_p, c_int32]),
     "sdden_destroy": (c_int, [c_void_p]),
     "sdden_last_error": (c_char_p, [c_void_p]),
+    "sdden_layernorm_workspace_bytes": (c_size_t, [c_int32, c_int32]),
+    "sdden_layernorm_forward": (c_int, [c_int32, c_int32, c_void_p, c_int32, c_int64, c_void_p, c_void_p, c_float, c_void_p, c_int32,
+                                        c_int64, c_void_p, c_void_p, c_void_p]),
+    "sdden_layernorm_backward": (c_int, [c_int32, c_int32, c_void_p, c_int32, c_int64, c_void_p, c_int32, c_int64, c_void_p, c_void_p,
+                                         c_void_p, c_void_p, c_int64, c_void_p, c_int64, c_void_p, c_void_p, c_void_p, c_size_t,
+                                         c_void_p]),
+    "sdden_gated_workspace_bytes": (c_size_t, [c_int32, c_int32, c_int32]),
+    "sdden_gated_forward": (c_int, [c_int32] * 4 + [c_void_p, c_int64] + [c_void_p] * 5 + [c_int32, c_int64] + [c_void_p] * 3),
+    "sdden_gated_backward": (c_int, [c_int32] * 4 + [c_void_p, c_int64, c_void_p, c_int64] + [c_void_p] * 6 + [c_int64]
+                             + [c_void_p] * 3 + [c_int32, c_void_p, c_size_t, c_void_p]),
 }
 
 _lib = None
@@ -429,6 +443,128 @@ class Denoiser:
             self.close()
         except Exception:
             pass
+
+
+# -- layers of row networks: functions of tensors on the current device, on its current stream
+_LAYER_TYPES = {torch.float32: SDDEN_F32, torch.bfloat16: SDDEN_BF16}
+
+
+def _rows(t: Optional[torch.Tensor], name: str, shape=None, types=(torch.float32, torch.bfloat16), allow_none: bool = False):
+    """(pointer, stride between rows) of a matrix whose rows are contiguous and need not follow each other."""
+    if t is None and allow_none:
+        return None, 0
+    if t is None or not t.is_cuda or t.device.index != torch._C._cuda_getDevice() or t.dtype not in types or t.dim() != 2:
+        raise SDError(f"{name}: need a matrix of {types} on the current device, got "
+                      + ("None" if t is None else f"{t.dtype} {tuple(t.shape)} on {t.device}"))
+    if shape is not None and tuple(t.shape) != tuple(shape):
+        raise SDError(f"{name}: need shape {tuple(shape)}, got {tuple(t.shape)}")
+    R, d = t.shape
+    if d > 1 and t.stride(1) != 1:
+        raise SDError(f"{name}: the elements of a row must be contiguous, got strides {t.stride()}")
+    stride = t.stride(0) if R > 1 else max(d, 1)
+    if stride < d:
+        raise SDError(f"{name}: rows overlap (stride {stride} of {d} columns)")
+    return t.data_ptr(), stride
+
+
+def _flat(t: Optional[torch.Tensor], name: str, shape, dtype, allow_none: bool = False) -> Optional[int]:
+    """Pointer of a contiguous tensor of this shape and type on the current device."""
+    if t is None and allow_none:
+        return None
+    if t is None or not t.is_cuda or t.device.index != torch._C._cuda_getDevice() or t.dtype is not dtype or not t.is_contiguous() \
+            or tuple(t.shape) != tuple(shape):
+        raise SDError(f"{name}: need a contiguous {dtype} tensor of shape {tuple(shape)} on the current device, got "
+                      + ("None" if t is None else f"{t.dtype} {tuple(t.shape)} on {t.device}"))
+    return t.data_ptr()
+
+
+def _scratch(t: Optional[torch.Tensor], name: str):
+    """(pointer, bytes) of a caller's workspace, any contiguous tensor."""
+    if t is None:
+        return None, 0
+    if not t.is_cuda or t.device.index != torch._C._cuda_getDevice() or not t.is_contiguous():
+        raise SDError(f"{name}: need a contiguous tensor on the current device")
+    return t.data_ptr(), t.numel() * t.element_size()
+
+
+def _layer_check(lib, rc: int, what: str):
+    if rc != 0:
+        raise SDError(f"{what} failed ({rc}): {lib.sdden_last_error(None).decode()}")
+
+
+def sdden_layernorm_workspace_bytes(R: int, d: int) -> int:
+    return int(load_library().sdden_layernorm_workspace_bytes(R, d))
+
+
+def sdden_layernorm_forward(x, weight, bias, eps: float, y, mean=None, rstd=None):
+    """x, y [R,d] fp32 or bf16, rows may lie apart; weight, bias [d] fp32 or None; mean, rstd [R] fp32 or both None."""
+    lib = load_library()
+    xp, xs = _rows(x, "x")
+    R, d = x.shape
+    yp, ys = _rows(y, "y", (R, d))
+    _layer_check(lib, lib.sdden_layernorm_forward(
+        R, d, xp, _LAYER_TYPES[x.dtype], xs, _flat(weight, "weight", (d,), torch.float32, True),
+        _flat(bias, "bias", (d,), torch.float32, True), eps, yp, _LAYER_TYPES[y.dtype], ys,
+        _flat(mean, "mean", (R,), torch.float32, True), _flat(rstd, "rstd", (R,), torch.float32, True), _stream()),
+        "sdden_layernorm_forward")
+
+
+def sdden_layernorm_backward(dy, x, weight, mean, rstd, dx, dweight=None, dbias=None, workspace=None, dres=None):
+    """dres and dx have x's type; dweight, dbias [d] fp32 or None; workspace: any tensor of sdden_layernorm_workspace_bytes."""
+    lib = load_library()
+    xp, xs = _rows(x, "x")
+    R, d = x.shape
+    dyp, dys = _rows(dy, "dy", (R, d))
+    dxp, dxs = _rows(dx, "dx", (R, d), (x.dtype,))
+    drp, drs = _rows(dres, "dres", (R, d), (x.dtype,), allow_none=True)
+    ws, nbytes = _scratch(workspace, "workspace")
+    _layer_check(lib, lib.sdden_layernorm_backward(
+        R, d, dyp, _LAYER_TYPES[dy.dtype], dys, xp, _LAYER_TYPES[x.dtype], xs, _flat(weight, "weight", (d,), torch.float32, True),
+        _flat(mean, "mean", (R,), torch.float32), _flat(rstd, "rstd", (R,), torch.float32), drp, drs, dxp, dxs,
+        _flat(dweight, "dweight", (d,), torch.float32, True), _flat(dbias, "dbias", (d,), torch.float32, True), ws, nbytes, _stream()),
+        "sdden_layernorm_backward")
+
+
+def sdden_gated_workspace_bytes(R: int, d: int, H: int) -> int:
+    return int(load_library().sdden_gated_workspace_bytes(R, d, H))
+
+
+def sdden_gated_forward(X, Wg, Wu, Wd, Y, hidden, gates=None, act: int = SDDEN_SILU, res=None):
+    """X [R,d], Wg, Wu [H,d], Wd [d,H], hidden [R,H] bf16; Y and res [R,d] fp32 or bf16; gates [2,R,H] fp32 or None."""
+    lib = load_library()
+    bf = torch.bfloat16
+    xp, xs = _rows(X, "X", types=(bf,))
+    R, d = X.shape
+    H = Wg.shape[0]
+    yp, ys = _rows(Y, "Y", (R, d))
+    rp, rs = _rows(res, "res", (R, d), (Y.dtype,), allow_none=True)
+    if res is not None and R > 1 and rs != ys:
+        raise SDError(f"res: its rows must lie as far apart as Y's ({ys}), got {rs}")
+    _layer_check(lib, lib.sdden_gated_forward(
+        R, d, H, act, xp, xs, _flat(Wg, "Wg", (H, d), bf), _flat(Wu, "Wu", (H, d), bf), _flat(Wd, "Wd", (d, H), bf), rp, yp,
+        _LAYER_TYPES[Y.dtype], ys, _flat(hidden, "hidden", (R, H), bf), _flat(gates, "gates", (2, R, H), torch.float32, True), _stream()),
+        "sdden_gated_forward")
+
+
+def sdden_gated_backward(dY, X, Wg, Wu, Wd, gates, hidden, dX, dWg, dWu, dWd, workspace, act: int = SDDEN_SILU):
+    """dX [R,d] bf16 or None; dWg, dWu [H,d], dWd [d,H] fp32 or bf16, or all None; workspace: any tensor of
+    sdden_gated_workspace_bytes."""
+    lib = load_library()
+    bf = torch.bfloat16
+    xp, xs = _rows(X, "X", types=(bf,))
+    R, d = X.shape
+    H = Wg.shape[0]
+    dyp, dys = _rows(dY, "dY", (R, d), (bf,))
+    dxp, dxs = _rows(dX, "dX", (R, d), (bf,), allow_none=True)
+    tw = torch.float32 if dWg is None else dWg.dtype
+    if tw not in _LAYER_TYPES:
+        raise SDError(f"dWg: need fp32 or bf16, got {tw}")
+    ws, nbytes = _scratch(workspace, "workspace")
+    _layer_check(lib, lib.sdden_gated_backward(
+        R, d, H, act, dyp, dys, xp, xs, _flat(Wg, "Wg", (H, d), bf), _flat(Wu, "Wu", (H, d), bf), _flat(Wd, "Wd", (d, H), bf),
+        _flat(gates, "gates", (2, R, H), torch.float32), _flat(hidden, "hidden", (R, H), bf), dxp, dxs,
+        _flat(dWg, "dWg", (H, d), tw, True), _flat(dWu, "dWu", (H, d), tw, True), _flat(dWd, "dWd", (d, H), tw, True),
+        _LAYER_TYPES[tw], ws, nbytes, _stream()), "sdden_gated_backward")
 
 
 def sd_measure_stream(src: Optional[torch.Tensor], dst: torch.Tensor, nbytes: int, mode: int, workgroups: int = 0):

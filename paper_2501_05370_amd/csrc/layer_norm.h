@@ -1,0 +1,346 @@
+// Layer norm over rows of d, forward and backward (sdden_layernorm_*).
+//
+//   xh = (x - mean) r,  r = 1 / sqrt(mean((x - mean)^2) + eps),  y = xh w + b
+//   g = dy w:  dx = r (g - mean(g) - xh mean(g xh)) [+ dres],   dw = sum over rows dy xh,   db = sum over rows dy
+//
+// Bound by HBM: each row is read once and kept in registers (E elements per thread of the TPR threads that share a row), so the
+// variance is the two-pass one, the sum of (x - mean)^2 around the finished mean, at no further traffic; everything between the
+// loads and the stores is fp32.  Rows longer than the widest register form are walked in three passes, out of L2.
+// The weights' gradients need a sum over all rows: a workgroup walks rows blockIdx, blockIdx + grid, ... with its columns'
+// sums in registers and leaves one partial row; reduce_partials_kernel adds those up in a fixed order (no atomics: the
+// same bits every time).
+#pragma once
+#include <hip/hip_runtime.h>
+
+#include <cstdint>
+
+#include "sd_lanes.h"
+
+namespace lnorm {
+
+struct Args {
+  int R, d;
+  const void *x, *dy, *dres;
+  void* y;                      // forward: y; backward: dx
+  int64_t ldx, lddy, lddres, ldy;
+  const float *w, *b;           // may be null
+  float* mean;                  // forward: out or null; backward: in
+  float* rstd;
+  float eps;
+  float* partial;               // backward: [2, grid, d] or null
+};
+
+template <int V, typename T>
+__device__ __forceinline__ void load(const T* p, float (&v)[V]) {
+  typedef T vec __attribute__((ext_vector_type(V), aligned(V * sizeof(T) < 16 ? V * sizeof(T) : 16)));
+  if constexpr (V == 1) {
+    v[0] = static_cast<float>(*p);
+  } else {
+    const vec t = *reinterpret_cast<const vec*>(p);
+#pragma unroll
+    for (int e = 0; e < V; ++e) v[e] = static_cast<float>(t[e]);
+  }
+}
+
+template <int V, typename T>
+__device__ __forceinline__ void store(T* p, const float (&v)[V]) {
+  typedef T vec __attribute__((ext_vector_type(V), aligned(V * sizeof(T) < 16 ? V * sizeof(T) : 16)));
+  if constexpr (V == 1) {
+    *p = static_cast<T>(v[0]);
+  } else {
+    vec t;
+#pragma unroll
+    for (int e = 0; e < V; ++e) t[e] = static_cast<T>(v[e]);
+    *reinterpret_cast<vec*>(p) = t;
+  }
+}
+
+template <int MASK>
+__device__ __forceinline__ float xor_add(float v) {
+  return v + __int_as_float(sdlane::lane_xor<MASK>(__float_as_int(v)));
+}
+__device__ __forceinline__ float wave_sum(float v) {
+  v = xor_add<1>(v);
+  v = xor_add<2>(v);
+  v = xor_add<4>(v);
+  v = xor_add<8>(v);
+  v = xor_add<16>(v);
+  return xor_add<32>(v);
+}
+
+// Sums of a and b over the TPR threads of a row; `slot` alternates between calls so that one barrier per call is enough.
+template <int TPR>
+__device__ __forceinline__ void row_sum2(float& a, float& b, float2 (&red)[2][16], int slot) {
+  a = wave_sum(a);
+  b = wave_sum(b);
+  if constexpr (TPR > 64) {
+    constexpr int NW = TPR / 64;
+    if ((threadIdx.x & 63) == 0) red[slot][threadIdx.x >> 6] = make_float2(a, b);
+    __syncthreads();
+    a = b = 0.f;
+#pragma unroll
+    for (int w = 0; w < NW; ++w) {
+      a += red[slot][w].x;
+      b += red[slot][w].y;
+    }
+  }
+}
+
+constexpr int threads_of(int tpr) { return tpr < 256 ? 256 : tpr; }
+
+// Columns of a thread: chunk c of V elements starts at (c * TPR + lane of the row) * V.
+template <int TPR, int E, int V, typename TX, typename TY>
+__global__ __launch_bounds__(threads_of(TPR)) void forward_kernel(Args p) {
+  constexpr int C = E / V, RPB = threads_of(TPR) / TPR;
+  __shared__ float2 red[2][16];
+  const int t = threadIdx.x % TPR;
+  const float inv_d = 1.0f / static_cast<float>(p.d);
+  float w[C][V], b[C][V];
+#pragma unroll
+  for (int c = 0; c < C; ++c) {
+    const int col = (c * TPR + t) * V;
+#pragma unroll
+    for (int e = 0; e < V; ++e) w[c][e] = 1.f, b[c][e] = 0.f;
+    if (col < p.d) {
+      if (p.w) load<V>(p.w + col, w[c]);
+      if (p.b) load<V>(p.b + col, b[c]);
+    }
+  }
+  for (int64_t r = static_cast<int64_t>(blockIdx.x) * RPB + threadIdx.x / TPR; r < p.R; r += static_cast<int64_t>(gridDim.x) * RPB) {
+    const TX* x = static_cast<const TX*>(p.x) + r * p.ldx;
+    float v[C][V];
+    float s = 0.f, unused = 0.f;
+#pragma unroll
+    for (int c = 0; c < C; ++c) {
+      const int col = (c * TPR + t) * V;
+      if (col < p.d) {
+        load<V>(x + col, v[c]);
+#pragma unroll
+        for (int e = 0; e < V; ++e) s += v[c][e];
+      }
+    }
+    row_sum2<TPR>(s, unused, red, 0);
+    const float mean = s * inv_d;
+    float q = 0.f;
+    unused = 0.f;
+#pragma unroll
+    for (int c = 0; c < C; ++c)
+      if ((c * TPR + t) * V < p.d) {
+#pragma unroll
+        for (int e = 0; e < V; ++e) {
+          v[c][e] -= mean;
+          q += v[c][e] * v[c][e];
+        }
+      }
+    row_sum2<TPR>(q, unused, red, 1);
+    const float rstd = 1.0f / sqrtf(q * inv_d + p.eps);
+    if (t == 0 && p.mean) {
+      p.mean[r] = mean;
+      p.rstd[r] = rstd;
+    }
+    TY* y = static_cast<TY*>(p.y) + r * p.ldy;
+#pragma unroll
+    for (int c = 0; c < C; ++c) {
+      const int col = (c * TPR + t) * V;
+      if (col < p.d) {
+#pragma unroll
+        for (int e = 0; e < V; ++e) v[c][e] = v[c][e] * rstd * w[c][e] + b[c][e];
+        store<V>(y + col, v[c]);
+      }
+    }
+  }
+}
+
+// Rows of any length: three walks over the row, the second and third out of L2.
+template <typename TX, typename TY>
+__global__ __launch_bounds__(1024) void forward_long_kernel(Args p) {
+  __shared__ float2 red[2][16];
+  for (int64_t r = blockIdx.x; r < p.R; r += gridDim.x) {
+    const TX* x = static_cast<const TX*>(p.x) + r * p.ldx;
+    TY* y = static_cast<TY*>(p.y) + r * p.ldy;
+    float s = 0.f, q = 0.f, unused = 0.f;
+    for (int c = threadIdx.x; c < p.d; c += 1024) s += static_cast<float>(x[c]);
+    row_sum2<1024>(s, unused, red, 0);
+    const float mean = s / static_cast<float>(p.d);
+    for (int c = threadIdx.x; c < p.d; c += 1024) {
+      const float v = static_cast<float>(x[c]) - mean;
+      q += v * v;
+    }
+    unused = 0.f;
+    row_sum2<1024>(q, unused, red, 1);
+    const float rstd = 1.0f / sqrtf(q / static_cast<float>(p.d) + p.eps);
+    if (threadIdx.x == 0 && p.mean) {
+      p.mean[r] = mean;
+      p.rstd[r] = rstd;
+    }
+    for (int c = threadIdx.x; c < p.d; c += 1024) {
+      const float w = p.w ? p.w[c] : 1.f, b = p.b ? p.b[c] : 0.f;
+      y[c] = static_cast<TY>((static_cast<float>(x[c]) - mean) * rstd * w + b);
+    }
+  }
+}
+
+// TY is dy's type, TX that of x, dres and dx.
+template <int TPR, int E, int V, typename TX, typename TY>
+__global__ __launch_bounds__(threads_of(TPR)) void backward_kernel(Args p) {
+  constexpr int C = E / V, RPB = threads_of(TPR) / TPR;
+  __shared__ float2 red[2][16];
+  __shared__ float fold[RPB > 1 ? (RPB - 1) * TPR * 2 : 1];
+  const int t = threadIdx.x % TPR, sub = threadIdx.x / TPR;
+  const float inv_d = 1.0f / static_cast<float>(p.d);
+  float w[C][V], dw[C][V], db[C][V];
+#pragma unroll
+  for (int c = 0; c < C; ++c) {
+    const int col = (c * TPR + t) * V;
+#pragma unroll
+    for (int e = 0; e < V; ++e) w[c][e] = 1.f, dw[c][e] = 0.f, db[c][e] = 0.f;
+    if (col < p.d && p.w) load<V>(p.w + col, w[c]);
+  }
+  int slot = 0;
+  for (int64_t r = static_cast<int64_t>(blockIdx.x) * RPB + sub; r < p.R; r += static_cast<int64_t>(gridDim.x) * RPB) {
+    const TX* x = static_cast<const TX*>(p.x) + r * p.ldx;
+    const TY* dy = static_cast<const TY*>(p.dy) + r * p.lddy;
+    const float mean = p.mean[r], rstd = p.rstd[r];
+    float xh[C][V], g[C][V];
+    float sg = 0.f, sgx = 0.f;
+#pragma unroll
+    for (int c = 0; c < C; ++c) {
+      const int col = (c * TPR + t) * V;
+      if (col < p.d) {
+        load<V>(x + col, xh[c]);
+        load<V>(dy + col, g[c]);
+      }
+    }
+#pragma unroll
+    for (int c = 0; c < C; ++c)
+      if ((c * TPR + t) * V < p.d) {
+#pragma unroll
+        for (int e = 0; e < V; ++e) {
+          xh[c][e] = (xh[c][e] - mean) * rstd;
+          dw[c][e] += g[c][e] * xh[c][e];
+          db[c][e] += g[c][e];
+          g[c][e] *= w[c][e];
+          sg += g[c][e];
+          sgx += g[c][e] * xh[c][e];
+        }
+      }
+    row_sum2<TPR>(sg, sgx, red, slot);
+    slot ^= 1;
+    sg *= inv_d;
+    sgx *= inv_d;
+    TX* dx = static_cast<TX*>(p.y) + r * p.ldy;
+    const TX* dres = p.dres ? static_cast<const TX*>(p.dres) + r * p.lddres : nullptr;
+#pragma unroll
+    for (int c = 0; c < C; ++c) {
+      const int col = (c * TPR + t) * V;
+      if (col < p.d) {
+        float o[V];
+#pragma unroll
+        for (int e = 0; e < V; ++e) o[e] = rstd * (g[c][e] - sg - xh[c][e] * sgx);
+        if (dres) {
+          float a[V];
+          load<V>(dres + col, a);
+#pragma unroll
+          for (int e = 0; e < V; ++e) o[e] += a[e];
+        }
+        store<V>(dx + col, o);
+      }
+    }
+  }
+  if (!p.partial) return;
+  float* pw = p.partial + static_cast<int64_t>(blockIdx.x) * p.d;
+  float* pb = pw + static_cast<int64_t>(gridDim.x) * p.d;
+#pragma unroll
+  for (int c = 0; c < C; ++c) {
+    const int col = (c * TPR + t) * V;
+#pragma unroll
+    for (int e = 0; e < V; ++e) {
+      float sw = dw[c][e], sb = db[c][e];
+      if constexpr (RPB > 1) {          // several rows at a time: their sums meet in LDS first
+        __syncthreads();
+        if (sub > 0) {
+          fold[((sub - 1) * TPR + t) * 2] = sw;
+          fold[((sub - 1) * TPR + t) * 2 + 1] = sb;
+        }
+        __syncthreads();
+        if (sub == 0) {
+#pragma unroll
+          for (int i = 0; i < RPB - 1; ++i) {
+            sw += fold[(i * TPR + t) * 2];
+            sb += fold[(i * TPR + t) * 2 + 1];
+          }
+        }
+      }
+      if (sub == 0 && col < p.d) {
+        pw[col + e] = sw;
+        pb[col + e] = sb;
+      }
+    }
+  }
+}
+
+// Rows of any length, dx only; the weights' gradients are those of long_partials_kernel.
+template <typename TX, typename TY>
+__global__ __launch_bounds__(1024) void backward_long_kernel(Args p) {
+  __shared__ float2 red[2][16];
+  int slot = 0;
+  for (int64_t r = blockIdx.x; r < p.R; r += gridDim.x) {
+    const TX* x = static_cast<const TX*>(p.x) + r * p.ldx;
+    const TY* dy = static_cast<const TY*>(p.dy) + r * p.lddy;
+    const float mean = p.mean[r], rstd = p.rstd[r];
+    float sg = 0.f, sgx = 0.f;
+    for (int c = threadIdx.x; c < p.d; c += 1024) {
+      const float g = static_cast<float>(dy[c]) * (p.w ? p.w[c] : 1.f);
+      sg += g;
+      sgx += g * ((static_cast<float>(x[c]) - mean) * rstd);
+    }
+    row_sum2<1024>(sg, sgx, red, slot);
+    slot ^= 1;
+    sg /= static_cast<float>(p.d);
+    sgx /= static_cast<float>(p.d);
+    TX* dx = static_cast<TX*>(p.y) + r * p.ldy;
+    const TX* dres = p.dres ? static_cast<const TX*>(p.dres) + r * p.lddres : nullptr;
+    for (int c = threadIdx.x; c < p.d; c += 1024) {
+      const float g = static_cast<float>(dy[c]) * (p.w ? p.w[c] : 1.f);
+      const float o = rstd * (g - sg - (static_cast<float>(x[c]) - mean) * rstd * sgx);
+      dx[c] = static_cast<TX>(o + (dres ? static_cast<float>(dres[c]) : 0.f));
+    }
+  }
+}
+
+// Partial row blockIdx.y of long rows' weight gradients: rows blockIdx.y, + gridDim.y, ... of 256 columns per workgroup.
+template <typename TX, typename TY>
+__global__ __launch_bounds__(256) void long_partials_kernel(Args p) {
+  const int c = blockIdx.x * 256 + threadIdx.x;
+  if (c >= p.d) return;
+  float sw = 0.f, sb = 0.f;
+  for (int64_t r = blockIdx.y; r < p.R; r += gridDim.y) {
+    const float v = static_cast<float>(static_cast<const TY*>(p.dy)[r * p.lddy + c]);
+    sw += v * ((static_cast<float>(static_cast<const TX*>(p.x)[r * p.ldx + c]) - p.mean[r]) * p.rstd[r]);
+    sb += v;
+  }
+  p.partial[static_cast<int64_t>(blockIdx.y) * p.d + c] = sw;
+  p.partial[static_cast<int64_t>(gridDim.y + blockIdx.y) * p.d + c] = sb;
+}
+
+// out[0..d) and out2[0..d): sums of the P partial rows; 64 columns x 16 shares of the rows per workgroup.
+__global__ __launch_bounds__(1024) void reduce_partials_kernel(const float* __restrict__ partial, int P, int d, float* __restrict__ dw,
+                                                               float* __restrict__ db) {
+  __shared__ float sum[16][64];
+  const int lane = threadIdx.x & 63, share = threadIdx.x >> 6, col = blockIdx.x * 64 + lane;
+  float* out = blockIdx.y ? db : dw;
+  if (!out) return;
+  float s = 0.f;
+  if (col < d)
+    for (int i = share; i < P; i += 16) s += partial[(static_cast<int64_t>(blockIdx.y) * P + i) * d + col];
+  sum[share][lane] = s;
+  __syncthreads();
+  if (share == 0 && col < d) {
+    s = 0.f;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) s += sum[i][lane];
+    out[col] = s;
+  }
+}
+
+}  // namespace lnorm

@@ -18,7 +18,7 @@
 #include "sdden_internal.h"
 
 namespace sdi {
-std::string g_den_create_error;
+thread_local std::string g_den_create_error;
 }
 
 namespace {

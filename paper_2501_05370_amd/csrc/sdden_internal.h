@@ -55,7 +55,7 @@ struct sdden {
 };
 
 namespace sdi {
-extern std::string g_den_create_error;
+extern thread_local std::string g_den_create_error;   // of calls that have no handle (yet): each thread's own
 
 // Rows to evaluate given the optional device-side chain count.
 __device__ __forceinline__ int active_rows(const int32_t* active, int rows_per_chain, int R) {

@@ -1,0 +1,260 @@
+// The layers of row networks behind sdden.h: layer norm (layer_norm.h) and the gated feed-forward block (layer_gemm.h), each
+// forward and backward.  Plain calls without a handle: the caller owns every buffer, nothing is kept between calls.
+#include <hip/hip_runtime.h>
+
+#include <algorithm>
+#include <cmath>
+
+#include "layer_gemm.h"
+#include "layer_norm.h"
+#include "sdden_internal.h"
+
+namespace {
+
+#define LAYER_ERR sdi::g_den_create_error
+
+bool type_ok(int32_t t) { return t == SDDEN_F32 || t == SDDEN_BF16; }
+bool aligned_to(const void* p, size_t n) { return (reinterpret_cast<uintptr_t>(p) & (n - 1)) == 0; }
+size_t size_of(int32_t t) { return t == SDDEN_F32 ? 4 : 2; }
+
+// ------------------------------------------------------------------------------------------------ layer norm
+// Threads per row and elements per thread by width: a wavefront up to 1024 columns (four rows to a workgroup), then the
+// smallest workgroup whose registers hold the row.
+enum Width { kWave, k256, k512, k1024, kLong };
+Width width_of(int d) { return d <= 1024 ? kWave : d <= 4096 ? k256 : d <= 12288 ? k512 : d <= 16384 ? k1024 : kLong; }
+
+// Partial rows of the weights' gradients: as many workgroups as walk the rows.
+int partial_rows(int R, int d) {
+  if (d > 16384) return std::min(R, 64);
+  if (d <= 1024) return std::min((R + 3) / 4, 1024);
+  return std::min(R, 512);
+}
+
+template <int V, typename TX, typename TY>
+void norm_forward(const lnorm::Args& a, hipStream_t st) {
+  const int R = a.R;
+  switch (width_of(a.d)) {
+    case kWave: hipLaunchKernelGGL((lnorm::forward_kernel<64, 16, V, TX, TY>), dim3(std::min((R + 3) / 4, 2048)), dim3(256), 0, st, a); break;
+    case k256: hipLaunchKernelGGL((lnorm::forward_kernel<256, 16, V, TX, TY>), dim3(std::min(R, 2048)), dim3(256), 0, st, a); break;
+    case k512: hipLaunchKernelGGL((lnorm::forward_kernel<512, 24, V, TX, TY>), dim3(std::min(R, 1024)), dim3(512), 0, st, a); break;
+    case k1024: hipLaunchKernelGGL((lnorm::forward_kernel<1024, 16, V, TX, TY>), dim3(std::min(R, 512)), dim3(1024), 0, st, a); break;
+    default: hipLaunchKernelGGL((lnorm::forward_long_kernel<TX, TY>), dim3(std::min(R, 512)), dim3(1024), 0, st, a); break;
+  }
+}
+
+template <int V, typename TX, typename TY>
+void norm_backward(const lnorm::Args& a, int P, hipStream_t st) {
+  switch (width_of(a.d)) {
+    case kWave: hipLaunchKernelGGL((lnorm::backward_kernel<64, 16, V, TX, TY>), dim3(P), dim3(256), 0, st, a); break;
+    case k256: hipLaunchKernelGGL((lnorm::backward_kernel<256, 16, V, TX, TY>), dim3(P), dim3(256), 0, st, a); break;
+    case k512: hipLaunchKernelGGL((lnorm::backward_kernel<512, 24, V, TX, TY>), dim3(P), dim3(512), 0, st, a); break;
+    case k1024: hipLaunchKernelGGL((lnorm::backward_kernel<1024, 16, V, TX, TY>), dim3(P), dim3(1024), 0, st, a); break;
+    default:
+      hipLaunchKernelGGL((lnorm::backward_long_kernel<TX, TY>), dim3(std::min(a.R, 512)), dim3(1024), 0, st, a);
+      if (a.partial) hipLaunchKernelGGL((lnorm::long_partials_kernel<TX, TY>), dim3((a.d + 255) / 256, P), dim3(256), 0, st, a);
+      break;
+  }
+}
+
+// Calls `go` with the vector width and the two types of the call as template arguments.
+template <typename F>
+void by_type(int vec, int32_t tx, int32_t ty, F&& go) {
+  using V1 = std::integral_constant<int, 1>;
+  using V4 = std::integral_constant<int, 4>;
+  using V8 = std::integral_constant<int, 8>;
+  const float f = 0.f;
+  const __bf16 b = static_cast<__bf16>(0.f);
+  if (tx == SDDEN_BF16 && ty == SDDEN_BF16) {
+    if (vec == 8) go(V8{}, b, b);
+    else go(V1{}, b, b);
+  } else if (vec == 1) {
+    if (tx == SDDEN_F32 && ty == SDDEN_F32) go(V1{}, f, f);
+    else if (tx == SDDEN_F32) go(V1{}, f, b);
+    else go(V1{}, b, f);
+  } else {
+    if (tx == SDDEN_F32 && ty == SDDEN_F32) go(V4{}, f, f);
+    else if (tx == SDDEN_F32) go(V4{}, f, b);
+    else go(V4{}, b, f);
+  }
+}
+
+// 16-byte loads (8 elements where both types are bf16, else 4) where every row and vector starts on such a boundary.
+int vector_width(int32_t d, int32_t tx, int32_t ty, std::initializer_list<int64_t> strides, std::initializer_list<const void*> ptrs) {
+  const int vec = tx == SDDEN_BF16 && ty == SDDEN_BF16 ? 8 : 4;
+  if (d % vec) return 1;
+  for (int64_t s : strides)
+    if (s % vec) return 1;
+  for (const void* p : ptrs)
+    if (!sdi::aligned16(p)) return 1;
+  return vec;
+}
+
+// ------------------------------------------------------------------------------------------------ gated block
+constexpr int64_t kMaxStride = int64_t{1} << 23;     // 128 rows of an operand stay within 32-bit offsets
+
+int check_gated(const char* what, int32_t R, int32_t d, int32_t H, int32_t act, const uint16_t* X, int64_t x_stride, const uint16_t* Wg,
+                const uint16_t* Wu, const uint16_t* Wd) {
+  if (R < 0 || d <= 0 || H <= 0 || (act != SDDEN_SILU && act != SDDEN_GELU) || !Wg || !Wu || !Wd || (R > 0 && !X))
+    return sdi::fail(LAYER_ERR, SD_ERR_ARG, "%s: bad argument", what);
+  if (d % 8 || H % 8)
+    return sdi::fail(LAYER_ERR, SD_ERR_UNSUPPORTED, "%s: d=%d and H=%d must be multiples of 8", what, d, H);
+  if (x_stride < d || x_stride % 8 || x_stride > kMaxStride || d > kMaxStride || H > kMaxStride)
+    return sdi::fail(LAYER_ERR, SD_ERR_ARG, "%s: x_stride=%lld must be a multiple of 8 from d=%d to %lld", what,
+                     static_cast<long long>(x_stride), d, static_cast<long long>(kMaxStride));
+  const int64_t tiles = (static_cast<int64_t>(R) + 127) / 128 * ((std::max(d, H) + 63) / 64), wtiles = (static_cast<int64_t>(d) + 127) / 128 * ((H + 127) / 128);
+  if (tiles > (1 << 28) || wtiles > (1 << 26))
+    return sdi::fail(LAYER_ERR, SD_ERR_UNSUPPORTED, "%s: R=%d rows of d=%d, H=%d are too many for one call", what, R, d, H);
+  if (!sdi::aligned16(X) || !sdi::aligned16(Wg) || !sdi::aligned16(Wu) || !sdi::aligned16(Wd))
+    return sdi::fail(LAYER_ERR, SD_ERR_ARG, "%s: X and the weights must be 16-byte aligned", what);
+  return SD_OK;
+}
+
+int done(const char* what, hipError_t e) {
+  if (e != hipSuccess) return sdi::fail(LAYER_ERR, SD_ERR_HIP, "%s: %s", what, hipGetErrorString(e));
+  return SD_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+size_t sdden_layernorm_workspace_bytes(int32_t R, int32_t d) {
+  if (R <= 0 || d <= 0) return 0;
+  return static_cast<size_t>(partial_rows(R, d)) * d * 2 * sizeof(float);
+}
+
+int sdden_layernorm_forward(int32_t R, int32_t d, const void* x, int32_t x_type, int64_t x_stride, const float* weight, const float* bias,
+                            float eps, void* y, int32_t y_type, int64_t y_stride, float* mean, float* rstd, void* stream) {
+  const char* what = "sdden_layernorm_forward";
+  if (R < 0 || d <= 0 || !type_ok(x_type) || !type_ok(y_type) || x_stride < d || y_stride < d || (R > 0 && (!x || !y)) || !mean != !rstd)
+    return sdi::fail(LAYER_ERR, SD_ERR_ARG, "%s: bad argument", what);
+  if (!(eps >= 0.f) || std::isinf(eps)) return sdi::fail(LAYER_ERR, SD_ERR_ARG, "%s: eps must be finite and not negative", what);
+  if (!aligned_to(x, size_of(x_type)) || !aligned_to(y, size_of(y_type)) || !aligned_to(weight, 4) || !aligned_to(bias, 4))
+    return sdi::fail(LAYER_ERR, SD_ERR_ARG, "%s: a pointer is not aligned to its element type", what);
+  if (R == 0) return SD_OK;
+  lnorm::Args a{};
+  a.R = R; a.d = d; a.x = x; a.ldx = x_stride; a.y = y; a.ldy = y_stride; a.w = weight; a.b = bias; a.mean = mean; a.rstd = rstd; a.eps = eps;
+  const int vec = vector_width(d, x_type, y_type, {x_stride, y_stride}, {x, y, weight, bias});
+  by_type(vec, x_type, y_type, [&](auto v, auto tx, auto ty) { norm_forward<decltype(v)::value, decltype(tx), decltype(ty)>(a, static_cast<hipStream_t>(stream)); });
+  return done(what, hipGetLastError());
+}
+
+int sdden_layernorm_backward(int32_t R, int32_t d, const void* dy, int32_t dy_type, int64_t dy_stride, const void* x, int32_t x_type,
+                             int64_t x_stride, const float* weight, const float* mean, const float* rstd, const void* dres,
+                             int64_t dres_stride, void* dx, int64_t dx_stride, float* dweight, float* dbias, void* workspace,
+                             size_t workspace_bytes, void* stream) {
+  const char* what = "sdden_layernorm_backward";
+  if (R < 0 || d <= 0 || !type_ok(x_type) || !type_ok(dy_type) || x_stride < d || dy_stride < d || dx_stride < d || (dres && dres_stride < d) ||
+      (R > 0 && (!x || !dy || !dx || !mean || !rstd)))
+    return sdi::fail(LAYER_ERR, SD_ERR_ARG, "%s: bad argument", what);
+  if (!aligned_to(x, size_of(x_type)) || !aligned_to(dx, size_of(x_type)) || !aligned_to(dres, size_of(x_type)) ||
+      !aligned_to(dy, size_of(dy_type)) || !aligned_to(weight, 4) || !aligned_to(workspace, 4))
+    return sdi::fail(LAYER_ERR, SD_ERR_ARG, "%s: a pointer is not aligned to its element type", what);
+  const bool grads = dweight || dbias;
+  if (grads && R > 0 && (!workspace || workspace_bytes < sdden_layernorm_workspace_bytes(R, d)))
+    return sdi::fail(LAYER_ERR, SD_ERR_WORKSPACE, "%s: dweight and dbias need %zu bytes of workspace, got %zu", what,
+                     sdden_layernorm_workspace_bytes(R, d), workspace ? workspace_bytes : 0);
+  lnorm::Args a{};
+  a.R = R; a.d = d; a.x = x; a.ldx = x_stride; a.dy = dy; a.lddy = dy_stride; a.dres = dres; a.lddres = dres ? dres_stride : 0;
+  a.y = dx; a.ldy = dx_stride; a.w = weight; a.mean = const_cast<float*>(mean); a.rstd = const_cast<float*>(rstd);
+  a.partial = grads ? static_cast<float*>(workspace) : nullptr;
+  hipStream_t st = static_cast<hipStream_t>(stream);
+  const int P = R > 0 ? partial_rows(R, d) : 0;
+  if (R > 0) {
+    const int vec = vector_width(d, x_type, dy_type, {x_stride, dy_stride, dx_stride, a.lddres}, {x, dy, dx, dres, weight});
+    by_type(vec, x_type, dy_type, [&](auto v, auto tx, auto ty) { norm_backward<decltype(v)::value, decltype(tx), decltype(ty)>(a, P, st); });
+  }
+  if (grads)
+    hipLaunchKernelGGL(lnorm::reduce_partials_kernel, dim3((d + 63) / 64, 2), dim3(1024), 0, st, a.partial, P, d, dweight, dbias);
+  return done(what, hipGetLastError());
+}
+
+size_t sdden_gated_workspace_bytes(int32_t R, int32_t d, int32_t H) {
+  if (R <= 0 || d <= 0 || H <= 0) return 0;
+  return static_cast<size_t>(R) * H * 2 * sizeof(uint16_t);            // dG, dU
+}
+
+int sdden_gated_forward(int32_t R, int32_t d, int32_t H, int32_t act, const uint16_t* X, int64_t x_stride, const uint16_t* Wg,
+                        const uint16_t* Wu, const uint16_t* Wd, const void* res, void* Y, int32_t y_type, int64_t y_stride,
+                        uint16_t* hidden, float* gates, void* stream) {
+  const char* what = "sdden_gated_forward";
+  if (int rc = check_gated(what, R, d, H, act, X, x_stride, Wg, Wu, Wd)) return rc;
+  if (!type_ok(y_type) || (R > 0 && (!Y || !hidden)) || y_stride < d || y_stride % 8 || y_stride > kMaxStride)
+    return sdi::fail(LAYER_ERR, SD_ERR_ARG, "%s: bad argument (Y, y_type, y_stride a multiple of 8 and at least d, hidden)", what);
+  if (!sdi::aligned16(Y) || !sdi::aligned16(res) || !sdi::aligned16(hidden) || !sdi::aligned16(gates))
+    return sdi::fail(LAYER_ERR, SD_ERR_ARG, "%s: Y, res, hidden and gates must be 16-byte aligned", what);
+  if (R == 0) return SD_OK;
+  hipStream_t st = static_cast<hipStream_t>(stream);
+  lgemm::Args a{};
+  a.problems = 1;
+  a.act = act;
+  lgemm::Problem& p = a.p[0];
+  p.A[0] = X; p.lda = x_stride; p.B[0] = Wg; p.B[1] = Wu; p.ldb = d; p.M = R; p.N = H; p.K = d; p.ranges = 1;
+  p.out = hidden; p.ldo = H;
+  if (gates) { p.gates[0] = gates; p.gates[1] = gates + static_cast<int64_t>(R) * H; }
+  hipError_t e = lgemm::launch<lgemm::kGate, lgemm::kAlong, lgemm::kAlong>(a, st);
+  if (e != hipSuccess) return done(what, e);
+  p = lgemm::Problem{};
+  p.A[0] = hidden; p.lda = H; p.B[0] = Wd; p.ldb = H; p.M = R; p.N = d; p.K = H; p.ranges = 1;
+  p.out = Y; p.ldo = y_stride; p.res = res; p.out_f32 = y_type == SDDEN_F32;
+  return done(what, lgemm::launch<lgemm::kStore, lgemm::kAlong, lgemm::kAlong>(a, st));
+}
+
+int sdden_gated_backward(int32_t R, int32_t d, int32_t H, int32_t act, const uint16_t* dY, int64_t dy_stride, const uint16_t* X,
+                         int64_t x_stride, const uint16_t* Wg, const uint16_t* Wu, const uint16_t* Wd, const float* gates,
+                         const uint16_t* hidden, uint16_t* dX, int64_t dx_stride, void* dWg, void* dWu, void* dWd, int32_t dw_type,
+                         void* workspace, size_t workspace_bytes, void* stream) {
+  const char* what = "sdden_gated_backward";
+  if (int rc = check_gated(what, R, d, H, act, X, x_stride, Wg, Wu, Wd)) return rc;
+  const bool weights = dWg || dWu || dWd;
+  if ((R > 0 && (!dY || !gates || !hidden)) || dy_stride < d || dy_stride % 8 || dy_stride > kMaxStride ||
+      (dX && (dx_stride < d || dx_stride % 8 || dx_stride > kMaxStride)) || !type_ok(dw_type) || (!dX && !weights))
+    return sdi::fail(LAYER_ERR, SD_ERR_ARG, "%s: bad argument (pointers, strides multiples of 8 and at least d, dw_type)", what);
+  if (weights && (!dWg || !dWu || !dWd))
+    return sdi::fail(LAYER_ERR, SD_ERR_ARG, "%s: dWg, dWu and dWd are computed together: give all three or none", what);
+  for (const void* q : {static_cast<const void*>(dY), static_cast<const void*>(gates), static_cast<const void*>(hidden),
+                        static_cast<const void*>(dX), static_cast<const void*>(dWg), static_cast<const void*>(dWu),
+                        static_cast<const void*>(dWd), static_cast<const void*>(workspace)})
+    if (!sdi::aligned16(q)) return sdi::fail(LAYER_ERR, SD_ERR_ARG, "%s: every buffer must be 16-byte aligned", what);
+  if (R > 0 && (!workspace || workspace_bytes < sdden_gated_workspace_bytes(R, d, H)))
+    return sdi::fail(LAYER_ERR, SD_ERR_WORKSPACE, "%s: needs %zu bytes of workspace, got %zu", what, sdden_gated_workspace_bytes(R, d, H),
+                     workspace ? workspace_bytes : 0);
+  hipStream_t st = static_cast<hipStream_t>(stream);
+  uint16_t* dG = static_cast<uint16_t*>(workspace);
+  uint16_t* dU = dG + static_cast<int64_t>(R) * H;
+  float* g = const_cast<float*>(gates);
+  if (R > 0) {
+    lgemm::Args a{};
+    a.problems = 1;
+    a.act = act;
+    lgemm::Problem& p = a.p[0];
+    p.A[0] = dY; p.lda = dy_stride; p.B[0] = Wd; p.ldb = H; p.M = R; p.N = H; p.K = d; p.ranges = 1;
+    p.out = dG; p.out2 = dU; p.ldo = H; p.gates[0] = g; p.gates[1] = g + static_cast<int64_t>(R) * H;
+    hipError_t e = lgemm::launch<lgemm::kGateGrad, lgemm::kAlong, lgemm::kAcross>(a, st);
+    if (e != hipSuccess) return done(what, e);
+    if (dX) {
+      p = lgemm::Problem{};
+      p.A[0] = dG; p.A[1] = dU; p.lda = H; p.B[0] = Wg; p.B[1] = Wu; p.ldb = d; p.M = R; p.N = d; p.K = H; p.ranges = 2;
+      p.out = dX; p.ldo = dx_stride;
+      e = lgemm::launch<lgemm::kStore, lgemm::kAlong, lgemm::kAcross>(a, st);
+      if (e != hipSuccess) return done(what, e);
+    }
+  }
+  if (weights) {
+    lgemm::Args a{};
+    a.problems = 3;
+    for (int i = 0; i < 3; ++i) {
+      lgemm::Problem& p = a.p[i];
+      p.K = R; p.ranges = 1; p.out_f32 = dw_type == SDDEN_F32;
+      if (i < 2) {
+        p.A[0] = i ? dU : dG; p.lda = H; p.B[0] = X; p.ldb = x_stride; p.M = H; p.N = d; p.out = i ? dWu : dWg; p.ldo = d;
+      } else {
+        p.A[0] = dY; p.lda = dy_stride; p.B[0] = hidden; p.ldb = H; p.M = d; p.N = H; p.out = dWd; p.ldo = H;
+      }
+    }
+    return done(what, lgemm::launch<lgemm::kStore, lgemm::kAcross, lgemm::kAcross>(a, st));
+  }
+  return SD_OK;
+}
+
+}  // extern "C"

@@ -1,0 +1,333 @@
+"""Layer norm and the gated feed-forward block against plain fp64 versions, forward and backward.
+
+Tolerances.  u = 2^-24 (fp32), b = 2^-8 (bf16, half a step relative to the value).  An element is compared with
+    rel * (its scale): rel * sum of |terms| of its own sum, so that cancellation is not charged to the kernel.
+Layer norm: a row's statistics are sums of d <= 40000 terms over at least 64 lanes and a tree, in all fewer than 64 + d / 64
+roundings one after the other; with |z| <= 8 and weights <= 2 the bound 1e-5 of the row's largest |y| covers d <= 4096
+(64 + 64 roundings of 2^-24 = 7.6e-6 at worst, and they do not all go one way); longer rows are walked by 1024 threads
+(40 roundings each).  bf16 outputs add b.
+Gated block: products of bf16 numbers are exact in fp32, their sums carry at most K roundings of u relative to sum |terms|
+(K <= 2048: 1.3e-4 at worst; 2e-5 holds in practice for random signs, but the bound is taken).  hidden, dG and dU are rounded
+to bf16 once (b of each term), outputs once more (b of the result).
+"""
+import numpy as np
+import pytest
+import torch
+
+from paper_2501_05370_amd import binding as B
+
+pytestmark = pytest.mark.gpu
+
+F32, BF = torch.float32, torch.bfloat16
+U16 = 2.0 ** -8           # half a bf16 step, relative
+
+
+def rows(gen, R, d, pad, dtype, scale=1.0, shift=0.0):
+    full = (torch.randn(R, d + pad, generator=gen, dtype=torch.float64) * scale + shift).to(dtype).cuda()
+    return full[:, :d]
+
+
+def out(R, d, pad, dtype):
+    """Rows of NaN with `pad` sentinels between them."""
+    full = torch.full((R, d + pad), float("nan"), dtype=dtype, device="cuda")
+    return full, full[:, :d]
+
+
+def norm_exact(x, w, b, eps):
+    mean = x.mean(1, keepdim=True)
+    rstd = (((x - mean) ** 2).mean(1, keepdim=True) + eps) ** -0.5
+    xh = (x - mean) * rstd
+    y = xh if w is None else xh * w
+    return mean, rstd, xh, y if b is None else y + b
+
+
+NORM = [  # R, d, pad, x, y, affine
+    (1, 1, 0, F32, F32, True), (3, 2, 0, BF, F32, True), (5, 63, 0, F32, BF, True), (4, 64, 0, BF, BF, True),
+    (7, 65, 3, F32, F32, False), (9, 1000, 8, BF, BF, True), (2, 1024, 0, F32, F32, True), (6, 1025, 0, F32, F32, True),
+    (33, 1028, 4, F32, BF, True), (3, 4096, 0, BF, BF, True), (3, 4097, 0, BF, BF, True), (2, 4100, 0, BF, F32, True),
+    (2, 12288, 0, F32, BF, True), (2, 12289, 0, F32, F32, True), (2, 16384, 8, BF, BF, False), (2, 16385, 1, F32, F32, True),
+    (3, 40000, 0, BF, BF, True), (2500, 96, 0, F32, F32, True), (700, 2056, 0, BF, BF, True), (9000, 17, 0, F32, F32, True),
+]
+
+
+@pytest.mark.parametrize("R,d,pad,tx,ty,affine", NORM)
+def test_norm_forward_and_backward(R, d, pad, tx, ty, affine):
+    gen = torch.Generator().manual_seed(R * 100003 + d)
+    x = rows(gen, R, d, pad, tx, 2.0, 0.7)
+    w = (1 + 0.2 * torch.randn(d, generator=gen)).cuda() if affine else None
+    b = torch.randn(d, generator=gen).cuda() if affine else None
+    eps = 1e-5
+    yfull, y = out(R, d, pad, ty)
+    mean, rstd = torch.full((R,), float("nan"), device="cuda"), torch.full((R,), float("nan"), device="cuda")
+    B.sdden_layernorm_forward(x, w, b, eps, y, mean, rstd)
+    xd = x.double().cpu()
+    wd, bd = (None if t is None else t.double().cpu() for t in (w, b))
+    emean, erstd, exh, ey = norm_exact(xd, wd, bd, eps)
+    scale = ey.abs().amax(1, keepdim=True).clamp_min(1e-3)
+    tol = 1e-5 + (U16 if ty is BF else 0)
+    assert ((y.double().cpu() - ey).abs() <= tol * scale + 1e-6).all()
+    assert yfull[:, d:].isnan().all(), "between the rows nothing is written"
+    assert torch.allclose(mean.double().cpu(), emean[:, 0], rtol=1e-5, atol=1e-5)
+    assert torch.allclose(rstd.double().cpu(), erstd[:, 0], rtol=1e-5)
+
+    dy, dres = rows(gen, R, d, pad, ty), rows(gen, R, d, 0, tx)
+    g64 = dy.double().cpu()
+    gw = g64 if wd is None else g64 * wd
+    for with_res in (True, False):
+        dxfull, dx = out(R, d, pad, tx)
+        ws = torch.empty(max(1, B.sdden_layernorm_workspace_bytes(R, d)), dtype=torch.uint8, device="cuda")
+        dw, db = torch.full((d,), float("nan"), device="cuda"), torch.full((d,), float("nan"), device="cuda")
+        B.sdden_layernorm_backward(dy, x, w, mean, rstd, dx, dw, db, ws, dres=dres if with_res else None)
+        edx = erstd * (gw - gw.mean(1, keepdim=True) - exh * (gw * exh).mean(1, keepdim=True))
+        s = (erstd * (gw.abs().amax(1, keepdim=True) * (1 + exh.abs().amax(1, keepdim=True))))
+        if with_res:
+            edx = edx + dres.double().cpu()
+            s = s + dres.double().cpu().abs()
+        assert ((dx.double().cpu() - edx).abs() <= 1e-5 * s + (U16 * edx.abs() if tx is BF else 0) + 1e-7).all()
+        assert dxfull[:, d:].isnan().all()
+        # at most R / 64 + 64 roundings of 2^-24 in a row, R <= 9000: 1.3e-5 of the sum of |terms|
+        terms = (g64 * exh).abs().sum(0)
+        assert ((dw.double().cpu() - (g64 * exh).sum(0)).abs() <= 2e-5 * terms + 1e-6).all()
+        assert ((db.double().cpu() - g64.sum(0)).abs() <= 2e-5 * g64.abs().sum(0) + 1e-6).all()
+        # only one of the two, and neither
+        dw2 = torch.full((d,), float("nan"), device="cuda")
+        B.sdden_layernorm_backward(dy, x, w, mean, rstd, dx, dw2, None, ws, dres=dres if with_res else None)
+        assert torch.equal(dw, dw2)
+        dx2 = torch.empty_like(dx)
+        B.sdden_layernorm_backward(dy, x, w, mean, rstd, dx2, dres=dres if with_res else None)
+        assert torch.equal(dx, dx2)
+
+
+def test_norm_gradient_against_differences():
+    """d/dt of sum(c * LN(x + t v)) by central differences in fp64 against <dx, v>, the kernels' dx."""
+    gen = torch.Generator().manual_seed(3)
+    R, d = 6, 130
+    x, c = rows(gen, R, d, 0, F32), rows(gen, R, d, 0, F32)
+    v = torch.randn(R, d, generator=gen, dtype=torch.float64)
+    w, b = (1 + 0.3 * torch.randn(d, generator=gen)).cuda(), torch.randn(d, generator=gen).cuda()
+    y, mean, rstd, dx = torch.empty_like(x), torch.empty(R, device="cuda"), torch.empty(R, device="cuda"), torch.empty_like(x)
+    B.sdden_layernorm_forward(x, w, b, 1e-5, y, mean, rstd)
+    B.sdden_layernorm_backward(c, x, w, mean, rstd, dx)
+    f = lambda t: (c.double().cpu() * norm_exact(x.double().cpu() + t * v, w.double().cpu(), b.double().cpu(), 1e-5)[3]).sum()
+    h = 1e-4
+    want = float((f(h) - f(-h)) / (2 * h))
+    got = float((dx.double().cpu() * v).sum())
+    assert abs(got - want) <= 1e-4 * float((dx.double().cpu() * v).abs().sum())
+
+
+def test_norm_of_constant_and_non_finite_rows():
+    x = torch.zeros(4, 256, device="cuda")
+    x[0] = 3.5
+    x[1, 7] = float("inf")
+    x[2, 9] = float("nan")
+    x[3] = torch.randn(256, device="cuda")
+    y = torch.empty_like(x)
+    B.sdden_layernorm_forward(x, None, None, 1e-5, y)
+    assert (y[0] == 0).all() and y[1].isnan().any() and y[2].isnan().all() and y[3].isfinite().all()
+
+
+def act(g, name):
+    if name == "silu":
+        s = torch.sigmoid(g)
+        return g * s, s + g * s * (1 - s)
+    P = torch.special.ndtr(g)
+    return g * P, P + g * torch.exp(-g * g / 2) / (2 * np.pi) ** 0.5
+
+
+ACT = {"silu": B.SDDEN_SILU, "gelu": B.SDDEN_GELU}
+GATED = [  # R, d, H, pad, act, y type, residual, weight-gradient type
+    (1, 8, 8, 0, "silu", F32, False, F32), (1, 64, 128, 0, "gelu", BF, True, BF), (2, 72, 40, 8, "silu", BF, False, BF),
+    (16, 256, 512, 0, "silu", F32, True, F32), (17, 136, 72, 16, "gelu", F32, True, BF), (31, 520, 248, 0, "silu", BF, True, BF),
+    (64, 1024, 64, 8, "silu", BF, False, F32), (65, 64, 1024, 0, "gelu", BF, False, BF), (127, 128, 128, 0, "silu", F32, False, F32),
+    (128, 200, 264, 0, "silu", BF, True, BF), (129, 512, 384, 24, "gelu", F32, True, F32), (300, 776, 520, 0, "silu", BF, False, BF),
+    (513, 256, 256, 0, "silu", BF, True, BF), (1000, 328, 648, 8, "silu", F32, False, F32), (257, 2048, 1032, 0, "silu", BF, False, BF),
+]
+
+
+def close(got, want, terms, roundings, dtype, K):
+    """|got - want| <= K u sum|terms| + (bf16 roundings inside) b sum|terms| + (own rounding) b |want|."""
+    tol = (K * 2.0 ** -24 + roundings * U16) * terms + (U16 * want.abs() if dtype is BF else 0) + 1e-6
+    bad = (got.double().cpu() - want).abs() > tol
+    assert not bad.any(), f"{int(bad.sum())} of {bad.numel()} off, worst {float(((got.double().cpu() - want).abs() / tol).max()):.2f} of the bound"
+
+
+@pytest.mark.parametrize("R,d,H,pad,name,ty,with_res,tw", GATED)
+def test_gated_forward_and_backward(R, d, H, pad, name, ty, with_res, tw):
+    gen = torch.Generator().manual_seed(R * 7919 + d * 31 + H)
+    x, dy = rows(gen, R, d, pad, BF), rows(gen, R, d, pad, BF)
+    wg, wu = (rows(gen, H, d, 0, BF, d ** -0.5) for _ in range(2))
+    wd = rows(gen, d, H, 0, BF, H ** -0.5)
+    res = rows(gen, R, d, pad, ty) if with_res else None
+    yfull, y = out(R, d, pad, ty)
+    hidden, gates = torch.empty(R, H, dtype=BF, device="cuda"), torch.empty(2, R, H, device="cuda")
+    B.sdden_gated_forward(x, wg, wu, wd, y, hidden, gates=gates, act=ACT[name], res=res)
+    X, G, U, D, DY = (t.double().cpu() for t in (x, wg, wu, wd, dy))
+    g, u = X @ G.T, X @ U.T
+    gt, ut = X.abs() @ G.abs().T, X.abs() @ U.abs().T
+    close(gates[0], g, gt, 0, F32, d)
+    close(gates[1], u, ut, 0, F32, d)
+    f, df = act(g, name)
+    a = f * u
+    # from here on: how far the sums that enter may be off moves what follows; relative errors below cover it at d <= 2048
+    errg = (d * 2.0 ** -24) * gt
+    erra = 1.2 * errg * u.abs() + f.abs() * (d * 2.0 ** -24) * ut
+    assert ((hidden.double().cpu() - a).abs() <= erra + U16 * a.abs() + 1e-6).all()
+    want = a @ D.T
+    slack = (erra @ D.abs().T)
+    if with_res:
+        want = want + res.double().cpu()
+    terms = a.abs() @ D.abs().T + (res.double().cpu().abs() if with_res else 0) + slack * 2.0 ** 8
+    close(y, want, terms, 1, ty, H)
+    assert yfull[:, d:].isnan().all()
+    # the same without the gates kept
+    y2, hidden2 = out(R, d, pad, ty)[1], torch.empty_like(hidden)
+    B.sdden_gated_forward(x, wg, wu, wd, y2, hidden2, act=ACT[name], res=res)
+    assert torch.equal(y, y2) and torch.equal(hidden, hidden2)
+
+    ws = torch.empty(max(16, B.sdden_gated_workspace_bytes(R, d, H)), dtype=torch.uint8, device="cuda")
+    dxfull, dx = out(R, d, pad, BF)
+    dwg, dwu, dwd = (torch.full(s, float("nan"), dtype=tw, device="cuda") for s in ((H, d), (H, d), (d, H)))
+    B.sdden_gated_backward(dy, x, wg, wu, wd, gates, hidden, dx, dwg, dwu, dwd, ws, act=ACT[name])
+    da, dat = DY @ D, DY.abs() @ D.abs()
+    dg, du = da * u * df, da * f
+    # terms of dG and dU: their own size plus what the fp32 sums behind them may be off, in units of b
+    dgt = dg.abs() + 2.0 ** 8 * (d * 2.0 ** -24) * (dat * u.abs() + da.abs() * ut + da.abs() * u.abs() * gt) * 1.2
+    dut = du.abs() + 2.0 ** 8 * (d * 2.0 ** -24) * (dat * f.abs() + da.abs() * gt) * 1.2
+    close(dx, dg @ G + du @ U, dgt @ G.abs() + dut @ U.abs(), 1, BF, 2 * H)
+    assert dxfull[:, d:].isnan().all()
+    close(dwg, dg.T @ X, dgt.T @ X.abs(), 1, tw, R)
+    close(dwu, du.T @ X, dut.T @ X.abs(), 1, tw, R)
+    hid = hidden.double().cpu()
+    close(dwd, DY.T @ hid, DY.T.abs() @ hid.abs(), 0, tw, R)
+    # only the rows' gradient, only the weights'
+    dx2 = torch.empty_like(dx)
+    B.sdden_gated_backward(dy, x, wg, wu, wd, gates, hidden, dx2, None, None, None, ws, act=ACT[name])
+    assert torch.equal(dx, dx2)
+    dws = [torch.empty_like(t) for t in (dwg, dwu, dwd)]
+    B.sdden_gated_backward(dy, x, wg, wu, wd, gates, hidden, None, *dws, ws, act=ACT[name])
+    assert all(torch.equal(p, q) for p, q in zip(dws, (dwg, dwu, dwd)))
+
+
+def test_gated_gradients_against_differences():
+    """d/dt of sum(c * Y(... + t v)) in fp64 against the kernels' gradients in that direction, for rows and each weight."""
+    gen = torch.Generator().manual_seed(11)
+    R, d, H = 24, 64, 96
+    x, c = rows(gen, R, d, 0, BF), rows(gen, R, d, 0, BF)
+    wg, wu, wd = rows(gen, H, d, 0, BF, d ** -0.5), rows(gen, H, d, 0, BF, d ** -0.5), rows(gen, d, H, 0, BF, H ** -0.5)
+    y, hidden, gates = torch.empty(R, d, device="cuda"), torch.empty(R, H, dtype=BF, device="cuda"), torch.empty(2, R, H, device="cuda")
+    ws = torch.empty(B.sdden_gated_workspace_bytes(R, d, H), dtype=torch.uint8, device="cuda")
+    grads = [torch.empty(R, d, dtype=BF, device="cuda")] + [torch.empty(s, device="cuda") for s in ((H, d), (H, d), (d, H))]
+    for name in ACT:
+        B.sdden_gated_forward(x, wg, wu, wd, y, hidden, gates=gates, act=ACT[name])
+        B.sdden_gated_backward(c, x, wg, wu, wd, gates, hidden, *grads, ws, act=ACT[name])
+        base = [t.double().cpu() for t in (x, wg, wu, wd)]
+
+        def f(ts):
+            return (c.double().cpu() * ((act(ts[0] @ ts[1].T, name)[0] * (ts[0] @ ts[2].T)) @ ts[3].T)).sum()
+
+        for i, gr in enumerate(grads):
+            v = torch.randn(base[i].shape, generator=gen, dtype=torch.float64)
+            h = 1e-5
+            up, down = list(base), list(base)
+            up[i], down[i] = base[i] + h * v, base[i] - h * v
+            want, got = float((f(up) - f(down)) / (2 * h)), float((gr.double().cpu() * v).sum())
+            # each of n gradient entries is off by at most 2 b of its size with either sign
+            assert abs(got - want) <= 2 * U16 * float((gr.double().cpu() * v).abs().sum())
+
+
+def test_gated_takes_nothing_from_other_rows():
+    """A row of NaN changes its own results and no other row's; a NaN behind the last column of strided rows none at all."""
+    gen = torch.Generator().manual_seed(5)
+    R, d, H = 70, 72, 136
+    x = rows(gen, R, d, 8, BF)
+    wg, wu, wd = rows(gen, H, d, 0, BF, 0.1), rows(gen, H, d, 0, BF, 0.1), rows(gen, d, H, 0, BF, 0.1)
+    y, y2 = torch.empty(R, d, device="cuda"), torch.empty(R, d, device="cuda")
+    hidden = torch.empty(R, H, dtype=BF, device="cuda")
+    B.sdden_gated_forward(x, wg, wu, wd, y, hidden)
+    full = torch.full((R, d + 8), float("nan"), dtype=BF, device="cuda")
+    full[:, :d] = x
+    B.sdden_gated_forward(full[:, :d], wg, wu, wd, y2, hidden)
+    assert torch.equal(y, y2)
+    full[33, :d] = float("nan")
+    B.sdden_gated_forward(full[:, :d], wg, wu, wd, y2, hidden)
+    keep = torch.arange(R, device="cuda") != 33
+    assert torch.equal(y[keep], y2[keep]) and y2[33].isnan().all()
+
+
+def test_no_rows():
+    d, H = 64, 128
+    e = torch.empty(0, d, dtype=BF, device="cuda")
+    w1, w2 = torch.randn(H, d, device="cuda").to(BF), torch.randn(d, H, device="cuda").to(BF)
+    hid, gates = torch.empty(0, H, dtype=BF, device="cuda"), torch.empty(2, 0, H, device="cuda")
+    B.sdden_gated_forward(e, w1, w1, w2, torch.empty_like(e), hid, gates=gates)
+    dws = [torch.full(s, 7.0, device="cuda") for s in ((H, d), (H, d), (d, H))]
+    B.sdden_gated_backward(e, e, w1, w1, w2, gates, hid, torch.empty_like(e), *dws, None)
+    assert all((t == 0).all() for t in dws)
+    n = torch.empty(0, device="cuda")
+    B.sdden_layernorm_forward(e, None, None, 1e-5, torch.empty_like(e), n, n)
+    dw, db = torch.full((d,), 7.0, device="cuda"), torch.full((d,), 7.0, device="cuda")
+    B.sdden_layernorm_backward(e, e, None, n, n, torch.empty_like(e), dw, db)
+    assert (dw == 0).all() and (db == 0).all()
+
+
+def test_layers_on_a_stream_and_in_a_graph():
+    """A whole step (norm, block, their backward passes) on a side stream, then captured and replayed on new inputs."""
+    gen = torch.Generator().manual_seed(9)
+    R, d, H = 130, 136, 264
+    wg, wu, wd = rows(gen, H, d, 0, BF, d ** -0.5), rows(gen, H, d, 0, BF, d ** -0.5), rows(gen, d, H, 0, BF, H ** -0.5)
+    w, b = torch.ones(d, device="cuda"), torch.zeros(d, device="cuda")
+    h, dh = rows(gen, R, d, 0, F32), rows(gen, R, d, 0, F32)
+    x, dyb = torch.empty(R, d, dtype=BF, device="cuda"), torch.empty(R, d, dtype=BF, device="cuda")
+    o = dict(mean=torch.empty(R, device="cuda"), rstd=torch.empty(R, device="cuda"), y=torch.empty(R, d, device="cuda"),
+             hidden=torch.empty(R, H, dtype=BF, device="cuda"), gates=torch.empty(2, R, H, device="cuda"),
+             dx=torch.empty(R, d, dtype=BF, device="cuda"), dwg=torch.empty(H, d, device="cuda"), dwu=torch.empty(H, d, device="cuda"),
+             dwd=torch.empty(d, H, device="cuda"), dh=torch.empty(R, d, device="cuda"), dw=torch.empty(d, device="cuda"),
+             db=torch.empty(d, device="cuda"))
+    ws1 = torch.empty(B.sdden_gated_workspace_bytes(R, d, H), dtype=torch.uint8, device="cuda")
+    ws2 = torch.empty(B.sdden_layernorm_workspace_bytes(R, d), dtype=torch.uint8, device="cuda")
+
+    def step():
+        B.sdden_layernorm_forward(h, w, b, 1e-5, x, o["mean"], o["rstd"])
+        B.sdden_gated_forward(x, wg, wu, wd, o["y"], o["hidden"], gates=o["gates"], res=h)
+        dyb.copy_(dh)
+        B.sdden_gated_backward(dyb, x, wg, wu, wd, o["gates"], o["hidden"], o["dx"], o["dwg"], o["dwu"], o["dwd"], ws1)
+        B.sdden_layernorm_backward(o["dx"], h, w, o["mean"], o["rstd"], o["dh"], o["dw"], o["db"], ws2, dres=dh)
+
+    step()
+    torch.cuda.synchronize()
+    want = {k: t.clone() for k, t in o.items()}
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        step()
+    side.synchronize()
+    assert all(torch.equal(o[k], want[k]) for k in o)
+    # the residual's derivative: the whole step against the formula in fp64, in the direction of h
+    hd, cd = h.double().cpu(), dh.double().cpu()
+    ts = [t.double().cpu() for t in (wg, wu, wd)]
+
+    def f(hh):
+        n = norm_exact(hh, None, None, 1e-5)[3]
+        return (cd * (hh + (act(n @ ts[0].T, "silu")[0] * (n @ ts[1].T)) @ ts[2].T)).sum()
+
+    v = torch.randn(R, d, generator=gen, dtype=torch.float64)
+    slope = float((f(hd + 1e-5 * v) - f(hd - 1e-5 * v)) / 2e-5)
+    got = o["dh"].double().cpu()
+    # the block's input, hidden, dG, dU, dY and dx are bf16: six roundings of b along the path, either sign
+    assert abs(float((got * v).sum()) - slope) <= 6 * U16 * float((got * v).abs().sum())
+
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step()
+    for seed in (1, 2, 3):
+        gen2 = torch.Generator().manual_seed(seed)
+        h.copy_(rows(gen2, R, d, 0, F32))
+        dh.copy_(rows(gen2, R, d, 0, F32))
+        step()
+        torch.cuda.synchronize()
+        want = {k: t.clone() for k, t in o.items()}
+        for t in o.values():
+            t.fill_(float("nan"))
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(o[k], want[k]) for k in o)
