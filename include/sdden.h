@@ -167,6 +167,22 @@ int sdden_gated_backward(int32_t R, int32_t d, int32_t H, int32_t act, const uin
                          int32_t dw_type, void* workspace, size_t workspace_bytes, void* stream);
 
 
+/* A matrix kept in 4 bits with one scale per group of inputs, and its product with rows:
+ *   Y[r,n] = sum_k X[r,k] (q[n,k] - 8) scale[n, k / group]  (+ bias[n])
+ * sdden_q4_create: q [N, ceil(K/2)] (row = output, two inputs per byte, the even one in the low half; values 0..15) and
+ * scale [N, ceil(K/group)] bf16 bit patterns: host, read during the call, which lays the matrix out on the current device in the
+ * kernels' order and waits for that.  group: 32, 64 or a multiple of 128 (K: one scale per row); N, K <= 2^20, any size.
+ * sdden_q4_eval: X [R,K] and Y [R,N] of SDDEN_F32 or SDDEN_BF16 with any stride, bias [N] fp32 or NULL: dev, on the matrix's
+ * device.  bf16 and fp32 rows enter exactly (an fp32 value as the sum of three bf16 ones: |x| < 2^127), sums are fp32, the output is
+ * rounded once.  A row's result depends on its position in the call and on R in the last bits of its sum, not on other rows.  A row
+ * with an infinity or a NaN gives NaN.  The handle is read only: any number of calls may use it at once, on any streams of its
+ * device, also captured ones, as long as it lives.  Errors: text in sdden_last_error(NULL). */
+typedef struct sdden_q4 sdden_q4;
+int sdden_q4_create(int32_t N, int32_t K, int32_t group, const uint8_t* q, const uint16_t* scale, sdden_q4** out);
+int sdden_q4_eval(const sdden_q4* m, int32_t R, const void* X, int32_t x_type, int64_t x_stride, const float* bias, void* Y,
+                  int32_t y_type, int64_t y_stride, void* stream);
+int sdden_q4_destroy(sdden_q4* m);
+
 #ifdef __cplusplus
 }
 #endif

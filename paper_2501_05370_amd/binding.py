@@ -100,6 +100,9 @@ _SIGNATURES = {
     "sdden_layernorm_backward": (c_int, [c_int32, c_int32, c_void_p, c_int32, c_int64, c_void_p, c_int32, c_int64, c_void_p, c_void_p,
                                          c_void_p, c_void_p, c_int64, c_void_p, c_int64, c_void_p, c_void_p, c_void_p, c_size_t,
                                          c_void_p]),
+    "sdden_q4_create": (c_int, [c_int32] * 3 + [c_void_p] * 2 + [POINTER(c_void_p)]),
+    "sdden_q4_eval": (c_int, [c_void_p, c_int32, c_void_p, c_int32, c_int64, c_void_p, c_void_p, c_int32, c_int64, c_void_p]),
+    "sdden_q4_destroy": (c_int, [c_void_p]),
     "sdden_gated_workspace_bytes": (c_size_t, [c_int32, c_int32, c_int32]),
     "sdden_gated_forward": (c_int, [c_int32] * 4 + [c_void_p, c_int64] + [c_void_p] * 5 + [c_int32, c_int64] + [c_void_p] * 3),
     "sdden_gated_backward": (c_int, [c_int32] * 4 + [c_void_p, c_int64, c_void_p, c_int64] + [c_void_p] * 6 + [c_int64]
@@ -565,6 +568,52 @@ def sdden_gated_backward(dY, X, Wg, Wu, Wd, gates, hidden, dX, dWg, dWu, dWd, wo
         _flat(gates, "gates", (2, R, H), torch.float32), _flat(hidden, "hidden", (R, H), bf), dxp, dxs,
         _flat(dWg, "dWg", (H, d), tw, True), _flat(dWu, "dWu", (H, d), tw, True), _flat(dWd, "dWd", (d, H), tw, True),
         _LAYER_TYPES[tw], ws, nbytes, _stream()), "sdden_gated_backward")
+
+
+class Q4Matrix:
+    """Owns one ``sdden_q4``: a matrix in 4 bits on the device that was current when it was created."""
+
+    def __init__(self, handle, N: int, K: int):
+        self._lib = load_library()
+        self._h = handle
+        self.N, self.K = N, K
+
+    @classmethod
+    def sdden_q4_create(cls, q, scale, K: int, group: int):
+        """q: uint8 [N, ceil(K/2)], two inputs per byte (the even one in the low half); scale: bf16 bit patterns, uint16 (or the
+        same as int16) [N, ceil(K/group)]."""
+        lib = load_library()
+        q, scale = np.ascontiguousarray(q), np.ascontiguousarray(scale)
+        if q.dtype != np.uint8 or scale.dtype not in (np.uint16, np.int16) or K <= 0 or group <= 0 or q.ndim != 2 \
+                or q.shape[1] != (K + 1) // 2 or scale.shape != (q.shape[0], -(-K // group)):
+            raise SDError(f"sdden_q4_create: need uint8 [N, ceil(K/2)] and 16-bit [N, ceil(K/group)] for K={K}, group={group}, got "
+                          f"{q.dtype} {q.shape} and {scale.dtype} {scale.shape}")
+        h = c_void_p()
+        rc = lib.sdden_q4_create(q.shape[0], K, group, q.ctypes.data, scale.ctypes.data, ctypes.byref(h))
+        _layer_check(lib, rc, "sdden_q4_create")
+        return cls(h, q.shape[0], K)
+
+    def sdden_q4_eval(self, X, Y, bias=None):
+        """X [R,K], Y [R,N] fp32 or bf16, rows may lie apart; bias [N] fp32 or None."""
+        xp, xs = _rows(X, "X")
+        if X.shape[1] != self.K:
+            raise SDError(f"X: need {self.K} columns, got {X.shape[1]}")
+        yp, ys = _rows(Y, "Y", (X.shape[0], self.N))
+        rc = self._lib.sdden_q4_eval(self._h, X.shape[0], xp, _LAYER_TYPES[X.dtype], xs, _flat(bias, "bias", (self.N,), torch.float32, True),
+                                     yp, _LAYER_TYPES[Y.dtype], ys, _stream())
+        if rc != 0:
+            _layer_check(self._lib, rc, "sdden_q4_eval")
+
+    def close(self):
+        if getattr(self, "_h", None):
+            self._lib.sdden_q4_destroy(self._h)
+            self._h = None
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
 
 
 def sd_measure_stream(src: Optional[torch.Tensor], dst: torch.Tensor, nbytes: int, mode: int, workgroups: int = 0):

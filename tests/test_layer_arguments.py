@@ -86,3 +86,30 @@ def test_errors_are_kept_per_thread():
     t.start()
     t.join()
     assert seen[0][0] == -1 and "gated" in seen[0][1] and "layernorm" in err()
+
+
+def q4_create(N=4, K=64, group=32, q=P, s=P, out=True):
+    h = ctypes.c_void_p()
+    return B.load_library().sdden_q4_create(N, K, group, q, s, ctypes.byref(h) if out else None)
+
+
+@pytest.mark.parametrize("kw,rc", [(dict(N=0), -1), (dict(K=0), -1), (dict(q=None), -1), (dict(s=None), -1), (dict(out=False), -1),
+                                   (dict(group=0), -5), (dict(group=-128), -5), (dict(group=16), -5), (dict(group=96), -5),
+                                   (dict(group=200), -5), (dict(N=(1 << 20) + 1), -5), (dict(K=(1 << 20) + 1), -5)])
+def test_q4_create_refuses(kw, rc):
+    assert q4_create(**kw) == rc and "sdden_q4_create" in err()
+
+
+def test_q4_calls_without_a_matrix():
+    lib = B.load_library()
+    assert lib.sdden_q4_eval(None, 1, P, 0, 64, None, P, 0, 64, None) == -1 and "sdden_q4_eval" in err()
+    assert lib.sdden_q4_destroy(None) == -1
+
+
+def test_q4_binding_checks_shapes():
+    import numpy as np
+    q, s = np.zeros((4, 33), np.uint8), np.zeros((4, 3), np.uint16)
+    for bad in (dict(q=q, scale=s, K=64, group=32), dict(q=q, scale=s, K=65, group=64), dict(q=q.astype(np.int8), scale=s, K=65, group=32),
+                dict(q=q, scale=s.astype(np.float32), K=65, group=32), dict(q=q, scale=s, K=65, group=0), dict(q=q[0], scale=s, K=65, group=32)):
+        with pytest.raises(B.SDError, match="sdden_q4_create"):
+            B.Q4Matrix.sdden_q4_create(**bad)
