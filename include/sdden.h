@@ -9,6 +9,10 @@
  *   lowrank  E[x0 | x_t] of N(mu, U U^T + s2 I): two skinny fp32 GEMMs in the eigenbasis of
  *            U U^T with a per-row diagonal gain in between
  *   mlp      3-layer SiLU MLP on [x ; sinusoidal(k)], bf16 weights, fp32 accumulation (bf16 MFMA)
+ *   mlp4     the same network with its matrices in 4 bits: a draft model of few bytes
+ *   gated    pre-norm residual gated blocks, bf16 weights, fp32 residual stream
+ *
+ * and, below them, the layers these are made of as calls of their own, with the backward passes that fit them.
  *
  * Conventions as in sd.h: "dev" pointers are caller-owned device memory, "host" pointers are read
  * during the create call only.  Rows with krow < 0 or krow >= T are skipped: nothing is computed
@@ -48,8 +52,24 @@ int sdden_mlp_create(int32_t d, int32_t H, int32_t E, const uint16_t* W1, const 
                      const uint16_t* W2, const float* b2, const uint16_t* W3, const float* b3,
                      int32_t T, int32_t Rmax, sdden** out);
 
+/* The same network with W1's first d rows, W2 and W3 kept in 4 bits with one bf16 scale per `group` inputs of an output (group:
+ * 32, 64 or a multiple of 128): scale = bf16(max |w| / 7), q = round(w / scale) + 8, quantised here from the bf16 weights; the
+ * time embedding and the biases stay as they are.  Rows and activations are bf16 as in sdden_mlp_create.  Any d and H up to 2^20.
+ * 4.1 to 4.5 bits per weight on the device.  Meant for the draft side of the independent drafter: a quarter of the target's bytes.
+ * A prediction does not depend on the call it is part of. */
+int sdden_mlp4_create(int32_t d, int32_t H, int32_t E, int32_t group, const uint16_t* W1, const float* b1, const uint16_t* W2,
+                      const float* b2, const uint16_t* W3, const float* b3, int32_t T, int32_t Rmax, sdden** out);
+
+/* A network of residual gated blocks:  h_0 = x + be + emb(k) We,  h_{l+1} = h_l + FF_l(LN_l(h_l)),  D(x, k) = h_blocks, with the
+ * layer norm and the gated block described further down.  We [E,d] bf16 (row = input feature), be [d]; norm_weight, norm_bias
+ * [blocks,d] fp32; Wg, Wu [blocks,H,d] and Wd [blocks,d,H] bf16, row = OUTPUT feature: host.  d and H multiples of 8.  The
+ * residual stream is fp32; the norm's output and the hidden rows are rounded to bf16. */
+int sdden_gated_create(int32_t d, int32_t H, int32_t E, int32_t blocks, int32_t act, const uint16_t* We, const float* be,
+                       const float* norm_weight, const float* norm_bias, float eps, const uint16_t* Wg, const uint16_t* Wu,
+                       const uint16_t* Wd, int32_t T, int32_t Rmax, sdden** out);
+
 /* Setup call: allocate the per-call scratch (row lists, intermediate activations) that
- * evaluations of up to Rmax rows need.  The gmm denoiser needs none; lowrank and mlp return
+ * evaluations of up to Rmax rows need.  The gmm denoiser needs none; the others return
  * SD_ERR_WORKSPACE from sdden_eval when R exceeds what was reserved.  May be called again with a
  * larger Rmax (not while evaluations are in flight). */
 int sdden_reserve(sdden* den, int32_t Rmax);
@@ -90,8 +110,8 @@ int sdden_run(sdden* den, sdden* draft_den, sd_ctx* ctx, int32_t B, const float*
 int sdden_set_active_count(sdden* den, const int32_t* count /*dev*/, int32_t rows_per_chain);
 
 /* Measurement aid: time the `which`-th kernel of every following sdden_eval with HIP events on
- * the evaluation's stream (gmm: 1 = posterior mean; lowrank: 1, 2 = the two GEMMs; mlp: 1..3 = the
- * three GEMMs; 0 = off, the default).  sdden_profile_collect waits for the recorded events, returns
+ * the evaluation's stream (gmm: 1 = posterior mean; lowrank: 1, 2 = the two GEMMs; mlp, mlp4: 1..3 = the
+ * three GEMMs; gated: 1 = the norms, 2, 3 = the blocks' first and last products; 0 = off, the default).  sdden_profile_collect waits for the recorded events, returns
  * the summed kernel time in ms and the number of timed launches, and starts a new collection.
  * Event objects are created on demand while profiling is on (never otherwise).
  * sdden_profile_min_rows restricts the timing to calls with R >= min_rows (default 0: every call),
@@ -174,7 +194,7 @@ int sdden_gated_backward(int32_t R, int32_t d, int32_t H, int32_t act, const uin
  * kernels' order and waits for that.  group: 32, 64 or a multiple of 128 (K: one scale per row); N, K <= 2^20, any size.
  * sdden_q4_eval: X [R,K] and Y [R,N] of SDDEN_F32 or SDDEN_BF16 with any stride, bias [N] fp32 or NULL: dev, on the matrix's
  * device.  bf16 and fp32 rows enter exactly (an fp32 value as the sum of three bf16 ones: |x| < 2^127), sums are fp32, the output is
- * rounded once.  A row's result depends on its position in the call and on R in the last bits of its sum, not on other rows.  A row
+ * rounded once.  Sums are taken in one order for every R: a row's result does not depend on the call it is part of.  A row
  * with an infinity or a NaN gives NaN.  The handle is read only: any number of calls may use it at once, on any streams of its
  * device, also captured ones, as long as it lives.  Errors: text in sdden_last_error(NULL). */
 typedef struct sdden_q4 sdden_q4;

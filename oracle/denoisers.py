@@ -10,6 +10,8 @@ definition:
                           (d x d) inverse taken through the Woodbury identity (an r x r solve).
 * ``MLPDenoiser``        a 3-layer SiLU MLP on [x ; sinusoidal(k)], evaluated in fp64 on the
                           bf16-rounded weights.
+* ``Q4MLPDenoiser``      the same network with its matrices replaced by their 4-bit values.
+* ``GatedDenoiser``      residual blocks of a layer norm and a gated feed-forward block, bf16-rounded weights.
 * ``GMMScore``           grad E for E = -log sum_m w_m N(x; mu_m, s^2 I)  (Langevin target).
 
 Every callable maps rows ``x [R, d]`` and integer chain steps ``k [R]`` to ``[R, d]``.
@@ -18,9 +20,11 @@ finite differences of log p_t, dense-solve comparison, hand-written loops on tin
 """
 from __future__ import annotations
 
+import math
+
 import numpy as np
 
-from workloads import GMMParams, LowRankGaussianParams, MLPParams, bf16_bits_to_f64
+from workloads import GatedParams, GMMParams, LowRankGaussianParams, MLPParams, Q4MLPParams, bf16_bits_to_f64, bf16_round_bits
 
 
 def _logsumexp(a: np.ndarray, axis: int) -> np.ndarray:
@@ -127,6 +131,51 @@ class MLPDenoiser:
         h1 = silu(inp @ self.W1 + self.p.b1)
         h2 = silu(h1 @ self.W2 + self.p.b2)
         return h2 @ self.W3 + self.p.b3
+
+
+_erf = np.vectorize(math.erf, otypes=[np.float64])
+
+
+def quantize4(W: np.ndarray, group: int) -> np.ndarray:
+    """The values that W [K, N] (row = input) stands for in 4 bits: per output and group of inputs scale = bf16(max |w| / 7),
+    w -> scale * clamp(round(w / scale), -8, 7), halves to even, all in fp32 as the library does it."""
+    K, N = W.shape
+    out = np.zeros((K, N))
+    for k0 in range(0, K, group):
+        w = W[k0:k0 + group].astype(np.float32)
+        s = bf16_bits_to_f64(bf16_round_bits(np.abs(w).max(axis=0) / np.float32(7.0))).astype(np.float32)
+        q = np.where(s > 0, np.rint(w / np.where(s > 0, s, np.float32(1.0))), np.float32(0.0))
+        out[k0:k0 + group] = np.clip(q, -8, 7).astype(np.float64) * s.astype(np.float64)
+    return out
+
+
+class Q4MLPDenoiser(MLPDenoiser):
+    """The MLP with its matrices (not the time embedding's rows) replaced by their 4-bit values."""
+
+    def __init__(self, q: Q4MLPParams):
+        super().__init__(q.p)
+        d = q.p.d
+        self.W1 = np.concatenate([quantize4(self.W1[:d], q.group), self.W1[d:]])
+        self.W2, self.W3 = quantize4(self.W2, q.group), quantize4(self.W3, q.group)
+
+
+class GatedDenoiser:
+    """h0 = x + be + emb(k) We;  h <- h + (f(n Wg^T) * (n Wu^T)) Wd^T,  n = LN(h), per block;  D = h."""
+
+    def __init__(self, p: GatedParams):
+        self.p = p
+        self.We, self.Wg, self.Wu, self.Wd = (bf16_bits_to_f64(w) for w in (p.We, p.Wg, p.Wu, p.Wd))
+
+    def __call__(self, x: np.ndarray, k: np.ndarray) -> np.ndarray:
+        p = self.p
+        h = np.asarray(x, dtype=np.float64) + p.be + sinusoidal_embedding(k, p.E) @ self.We
+        for l in range(self.Wg.shape[0]):
+            mean = h.mean(axis=1, keepdims=True)
+            n = (h - mean) / np.sqrt(((h - mean) ** 2).mean(axis=1, keepdims=True) + p.eps) * p.norm_weight[l] + p.norm_bias[l]
+            g = n @ self.Wg[l].T
+            f = silu(g) if p.act == 0 else g * 0.5 * (1.0 + _erf(g / np.sqrt(2.0)))
+            h = h + (f * (n @ self.Wu[l].T)) @ self.Wd[l].T
+        return h
 
 
 class GMMScore:

@@ -84,6 +84,8 @@ _SIGNATURES = {
                                      POINTER(c_void_p)]),
     "sdden_mlp_create": (c_int, [c_int32, c_int32, c_int32] + [c_void_p] * 6 + [c_int32, c_int32,
                                                                                POINTER(c_void_p)]),
+    "sdden_mlp4_create": (c_int, [c_int32] * 4 + [c_void_p] * 6 + [c_int32, c_int32, POINTER(c_void_p)]),
+    "sdden_gated_create": (c_int, [c_int32] * 5 + [c_void_p] * 4 + [c_float] + [c_void_p] * 3 + [c_int32, c_int32, POINTER(c_void_p)]),
     "sdden_reserve": (c_int, [c_void_p, c_int32]),
     "sdden_eval": (c_int, [c_void_p, c_int32, c_void_p, c_void_p, c_void_p, c_void_p]),
     "sdden_run": (c_int, [c_void_p, c_void_p, c_void_p, c_int32] + [c_void_p] * 8),
@@ -384,6 +386,36 @@ class Denoiser:
         den = cls(cls._created(rc, h, "sdden_mlp_create"), p.d)
         den.wants_bf16 = True                      # first layer reads bf16: sdden_eval_mirror saves a conversion pass
         return den
+
+    @classmethod
+    def sdden_mlp4_create(cls, p, group: int, T: int, Rmax: int):
+        """p: the bf16 network, as for ``sdden_mlp_create``; its matrices are quantised by the library."""
+        lib = load_library()
+        W1, W2, W3 = (_host(v, np.uint16) for v in (p.W1, p.W2, p.W3))
+        b1, b2, b3 = (_host(v, np.float32) for v in (p.b1, p.b2, p.b3))
+        if W1.shape != (p.d + p.E, p.H) or W2.shape != (p.H, p.H) or W3.shape != (p.H, p.d):
+            raise SDError(f"sdden_mlp4_create: weights of shapes {W1.shape}, {W2.shape}, {W3.shape} do not fit d={p.d}, H={p.H}, E={p.E}")
+        h = c_void_p()
+        rc = lib.sdden_mlp4_create(p.d, p.H, p.E, group, W1.ctypes.data, b1.ctypes.data, W2.ctypes.data, b2.ctypes.data,
+                                   W3.ctypes.data, b3.ctypes.data, T, Rmax, ctypes.byref(h))
+        den = cls(cls._created(rc, h, "sdden_mlp4_create"), p.d)
+        den.wants_bf16 = True
+        return den
+
+    @classmethod
+    def sdden_gated_create(cls, p, T: int, Rmax: int):
+        """p: ``workloads.GatedParams`` (or the same fields)."""
+        lib = load_library()
+        We, Wg, Wu, Wd = (_host(v, np.uint16) for v in (p.We, p.Wg, p.Wu, p.Wd))
+        be, nw, nb = (_host(v, np.float32) for v in (p.be, p.norm_weight, p.norm_bias))
+        L, H, d = Wg.shape
+        if Wu.shape != (L, H, d) or Wd.shape != (L, d, H) or nw.shape != (L, d) or nb.shape != (L, d) or be.shape != (d,) \
+                or We.ndim != 2 or We.shape[1] != d:
+            raise SDError("sdden_gated_create: the parameters' shapes do not fit each other")
+        h = c_void_p()
+        rc = lib.sdden_gated_create(d, H, We.shape[0], L, p.act, We.ctypes.data, be.ctypes.data, nw.ctypes.data, nb.ctypes.data, p.eps,
+                                    Wg.ctypes.data, Wu.ctypes.data, Wd.ctypes.data, T, Rmax, ctypes.byref(h))
+        return cls(cls._created(rc, h, "sdden_gated_create"), d)
 
     def _check(self, rc, what):
         if rc != 0:

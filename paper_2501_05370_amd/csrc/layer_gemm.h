@@ -52,6 +52,8 @@ struct Problem {
   float* gates[2];        // kGate (out, or null) and kGateGrad (in): g and u
   const void* res;        // kStore: added to C, or null; same type and stride as out
   int64_t ldo;            // elements between rows of out / out2
+  const int32_t* count;   // rows that count, at most M (device; null: M)
+  const int32_t* rowidx;  // kStore: row m of C goes to row rowidx[m] of out (null: m); res is in the order of C
   int out_f32;            // kStore: type of out and res
   int tiles_m, tiles_n, tile0;
 };
@@ -144,7 +146,7 @@ __device__ __forceinline__ bf16x8 read_fragment(const unsigned char* panel, int 
 // One row's four consecutive columns; kGate: g and u of the same four hidden columns.
 template <int EPI>
 __device__ __forceinline__ void store4(const Problem& p, int act, int64_t m, int n, f32x4 c, f32x4 c2) {
-  const int64_t at = m * p.ldo + n;
+  int64_t at = m * p.ldo + n;
   if constexpr (EPI == kGate) {
     if (p.gates[0]) {
       const int64_t gat = m * p.N + n;
@@ -173,12 +175,14 @@ __device__ __forceinline__ void store4(const Problem& p, int act, int64_t m, int
     *reinterpret_cast<u32x2*>(static_cast<uint16_t*>(p.out) + at) = pack_bf16(dg);
     *reinterpret_cast<u32x2*>(static_cast<uint16_t*>(p.out2) + at) = pack_bf16(du);
   } else {
+    const int64_t rat = at;
+    if (p.rowidx) at = static_cast<int64_t>(p.rowidx[m]) * p.ldo + n;
     if (p.out_f32) {
-      if (p.res) c += *reinterpret_cast<const f32x4*>(static_cast<const float*>(p.res) + at);
+      if (p.res) c += *reinterpret_cast<const f32x4*>(static_cast<const float*>(p.res) + rat);
       *reinterpret_cast<f32x4*>(static_cast<float*>(p.out) + at) = c;
     } else {
       if (p.res) {
-        const bf16x4 r = *reinterpret_cast<const bf16x4*>(static_cast<const uint16_t*>(p.res) + at);
+        const bf16x4 r = *reinterpret_cast<const bf16x4*>(static_cast<const uint16_t*>(p.res) + rat);
 #pragma unroll
         for (int e = 0; e < 4; ++e) c[e] += static_cast<float>(r[e]);
       }
@@ -227,6 +231,8 @@ __global__ __launch_bounds__(256) void kernel128(Args a) {
   const Problem& p = a.p[which];
   const int t = threadIdx.x, lane = t & 63, wave = __builtin_amdgcn_readfirstlane(t >> 6);
   const int wm = wave >> 1, wn = wave & 1, l16 = lane & 15, lq = lane >> 4;
+  const int M = p.count ? (*p.count < p.M ? *p.count : p.M) : p.M;
+  if (tm * 2 * HB >= M) return;
   const int m0 = tm * 2 * HB, n0 = tn * (EPI == kGate ? HB : 2 * HB);
   const int slices = (p.K + 63) / 64, nk = slices * p.ranges;
 
@@ -236,14 +242,14 @@ __global__ __launch_bounds__(256) void kernel128(Args a) {
   int i0, valid;
   if (!is_b) {
     i0 = m0 + wave * HB;
-    valid = p.M - i0;
+    valid = M - i0;
   } else {
     i0 = EPI == kGate ? n0 : n0 + (wave - 2) * HB;
     valid = p.N - i0;
   }
   if (valid <= 0) {               // a half panel past the end repeats the tile's first rows
     i0 = is_b ? n0 : m0;
-    valid = (is_b ? p.N : p.M) - i0;
+    valid = (is_b ? p.N : M) - i0;
   }
   const uint16_t* src[2];
   src[0] = is_b ? (EPI == kGate ? p.B[wave - 2] : p.B[0]) : p.A[0];
@@ -308,7 +314,7 @@ __global__ __launch_bounds__(256) void kernel128(Args a) {
 #pragma unroll
     for (int ra = 0; ra < 2; ++ra) {
       const int m = m0 + i * HB + wm * 32 + ra * 16 + l16;
-      if (m >= p.M) continue;
+      if (m >= M) continue;
 #pragma unroll
       for (int rb = 0; rb < 2; ++rb) {
         const int n = n0 + wn * 32 + rb * 16 + 4 * lq;

@@ -28,6 +28,7 @@ struct Args {
   float* rstd;
   float eps;
   float* partial;               // backward: [2, grid, d] or null
+  const int32_t* count;         // forward: rows that count, at most R (device; null: R)
 };
 
 template <int V, typename T>
@@ -91,6 +92,7 @@ constexpr int threads_of(int tpr) { return tpr < 256 ? 256 : tpr; }
 // Columns of a thread: chunk c of V elements starts at (c * TPR + lane of the row) * V.
 template <int TPR, int E, int V, typename TX, typename TY>
 __global__ __launch_bounds__(threads_of(TPR)) void forward_kernel(Args p) {
+  if (p.count) p.R = *p.count < p.R ? *p.count : p.R;
   constexpr int C = E / V, RPB = threads_of(TPR) / TPR;
   __shared__ float2 red[2][16];
   const int t = threadIdx.x % TPR;
@@ -154,6 +156,7 @@ __global__ __launch_bounds__(threads_of(TPR)) void forward_kernel(Args p) {
 // Rows of any length: three walks over the row, the second and third out of L2.
 template <typename TX, typename TY>
 __global__ __launch_bounds__(1024) void forward_long_kernel(Args p) {
+  if (p.count) p.R = *p.count < p.R ? *p.count : p.R;
   __shared__ float2 red[2][16];
   for (int64_t r = blockIdx.x; r < p.R; r += gridDim.x) {
     const TX* x = static_cast<const TX*>(p.x) + r * p.ldx;

@@ -9,6 +9,8 @@
 //   the -8      the sum of a group starts from -8 sum(x), which a matrix instruction with a constant operand leaves in just the
 //               layout of the sum; one such chain serves every 16 columns a wavefront computes on the same rows
 //   fp32 rows   are three bf16 pieces (8 + 8 + 8 bits: exact) that take three rows of the tile; the epilogue adds them up
+// The order of a sum is the same everywhere: within a group along k, the groups of the blocks b = i, i + 8, i + 16, ... (128 k
+// each) in that order for i = 0 .. 7, and then those eight sums; so a row's result does not depend on the call it is part of.
 //
 // Layout (made once, at create): 16 columns x 128 k are one block of 1 KiB, in which lane (l16, lq) finds its 16 bytes: dword
 // j holds column l16, k = 32 j + 8 lq .. + 7, elements 0..3 in the low halves of its bytes and 4..7 in the high ones.  The blocks
@@ -64,6 +66,14 @@ __device__ __forceinline__ bf16x8 unpack(uint32_t w) {
 __device__ __forceinline__ f32x4 scales4(u32x2 s) {
   return f32x4{__uint_as_float(s[0] << 16), __uint_as_float(s[0] & 0xFFFF0000u), __uint_as_float(s[1] << 16), __uint_as_float(s[1] & 0xFFFF0000u)};
 }
+
+__device__ __forceinline__ f32x4 add_scaled(f32x4 a, f32x4 s, f32x4 c) {
+#pragma unroll
+  for (int e = 0; e < 4; ++e) a[e] = __builtin_fmaf(s[e], c[e], a[e]);
+  return a;
+}
+
+constexpr int kShares = 8;       // partial sums of an output, see the top
 
 // Eight values of a row from k on; past K they are 0.
 template <int ROWS>
@@ -177,7 +187,7 @@ __device__ __forceinline__ bf16x8 minus8() {
 // Weights are requested two blocks ahead, rows one, in registers: there is no barrier in the loop.
 template <int MT, int GPB, int ROWS>
 __global__ __launch_bounds__(512) void few_kernel(Args p) {
-  constexpr int NW = 8, kPanel = 16 * MT * 256, PIECES = pieces(ROWS), kRealRows = 16 * MT / PIECES;
+  constexpr int NW = kShares, kPanel = 16 * MT * 256, PIECES = pieces(ROWS), kRealRows = 16 * MT / PIECES;
   constexpr int kChunks = (kRealRows * 16 + 63) / 64;       // chunks of a block per lane
   __shared__ __align__(1024) unsigned char lds[NW * kPanel];
   const int t = threadIdx.x, lane = t & 63, wave = __builtin_amdgcn_readfirstlane(t >> 6), l16 = lane & 15, lq = lane >> 4;
@@ -248,7 +258,7 @@ __global__ __launch_bounds__(512) void few_kernel(Args p) {
         for (int j = 0; j < J; ++j) c = __builtin_amdgcn_mfma_f32_16x16x32_bf16(m8, xf[j], c, 0, 0, 0);
 #pragma unroll
         for (int j = 0; j < J; ++j) c = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wf[j], xf[j], c, 0, 0, 0);
-        acc[i] += s * c;
+        acc[i] = add_scaled(acc[i], s, c);
       }
     }
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
@@ -272,9 +282,12 @@ __global__ __launch_bounds__(512) void few_kernel(Args p) {
     const int r = e >> 2, q = e & 3;
     f32x4 c{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-    for (int i = 0; i < NW; ++i)
+    for (int k = 0; k < PIECES; ++k) {
+      f32x4 piece{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-      for (int k = 0; k < PIECES; ++k) c += sums[(i * 16 * MT + PIECES * r + k) * 4 + q];
+      for (int i = 0; i < NW; ++i) piece += sums[(i * 16 * MT + PIECES * r + k) * 4 + q];
+      c += piece;
+    }
     const int n = 16 * tile + 4 * q;
     if (n < p.N) finish4(p, row0 + r, n, c);
   }
@@ -331,21 +344,23 @@ __global__ __launch_bounds__(256) void many_kernel(Args p) {
       for (int g = 0; g < GPB; ++g) s[i][g] = *reinterpret_cast<const u32x2*>(p.S + (at * GPB + g) * 16 + 4 * lq);
     }
   };
-  f32x4 acc[4][4];
+  f32x4 acc[4][4], total[4][4];
 #pragma unroll
-  for (int i = 0; i < 16; ++i) acc[i >> 2][i & 3] = f32x4{0.f, 0.f, 0.f, 0.f};
+  for (int i = 0; i < 16; ++i) acc[i >> 2][i & 3] = total[i >> 2][i & 3] = f32x4{0.f, 0.f, 0.f, 0.f};
   fetch_rows(0);
   fetch_weights(0, w, s);
   put_rows(0);
   __syncthreads();
   const bf16x8 m8 = minus8();
-  for (int b = 0; b < p.kblocks; ++b) {
-    const bool more = b + 1 < p.kblocks;
+  for (int b = 0, step = 0; step < p.kblocks; ++step) {
+    int next = b + kShares;                      // the last block of a share: its sum is complete
+    const bool share_ends = next >= p.kblocks, more = step + 1 < p.kblocks;
+    if (share_ends) next = b % kShares + 1;
     if (more) {
-      fetch_rows(b + 1);
-      fetch_weights(b + 1, wnext, snext);
+      fetch_rows(next);
+      fetch_weights(next, wnext, snext);
     }
-    const unsigned char* panel = lds + (b & 1) * kPanel;
+    const unsigned char* panel = lds + (step & 1) * kPanel;
 #pragma unroll
     for (int g = 0; g < GPB; ++g) {
       constexpr int J = 4 / GPB;
@@ -374,11 +389,21 @@ __global__ __launch_bounds__(256) void many_kernel(Args p) {
 #pragma unroll
           for (int i = 0; i < 4; ++i) c[i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wf[j], xf[i][j], c[i], 0, 0, 0);
 #pragma unroll
-        for (int i = 0; i < 4; ++i) acc[i][n] += sc * c[i];
+        for (int i = 0; i < 4; ++i) acc[i][n] = add_scaled(acc[i][n], sc, c[i]);
       }
     }
+    if (share_ends) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+#pragma unroll
+        for (int n = 0; n < 4; ++n) {
+          total[i][n] += acc[i][n];
+          acc[i][n] = f32x4{0.f, 0.f, 0.f, 0.f};
+        }
+    }
+    b = next;
     if (more) {
-      put_rows((b + 1) & 1);
+      put_rows((step + 1) & 1);
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
         w[i] = wnext[i];
@@ -396,7 +421,7 @@ __global__ __launch_bounds__(256) void many_kernel(Args p) {
 #pragma unroll
       for (int n = 0; n < 4; ++n) {
         const int col = (ct * 8 + wn * 4 + n) * 16 + 4 * lq;
-        if (col < p.N) finish4(p, row0 + r, col, acc[i][n]);
+        if (col < p.N) finish4(p, row0 + r, col, total[i][n]);
       }
     }
   } else {
@@ -405,7 +430,7 @@ __global__ __launch_bounds__(256) void many_kernel(Args p) {
 #pragma unroll
     for (int i = 0; i < 4; ++i)
 #pragma unroll
-      for (int n = 0; n < 4; ++n) sums[(wm * 64 + 16 * i + l16) * 32 + (wn * 4 + n) * 4 + lq] = acc[i][n];
+      for (int n = 0; n < 4; ++n) sums[(wm * 64 + 16 * i + l16) * 32 + (wn * 4 + n) * 4 + lq] = total[i][n];
     __syncthreads();
     for (int e = t; e < rows * 32; e += 256) {
       const int r = e >> 5, q = e & 31, col = ct * 128 + 4 * q;

@@ -4,10 +4,15 @@
 
 #include <algorithm>
 #include <cmath>
+#include <exception>
+#include <memory>
+#include <vector>
 
 #include "layer_gemm.h"
 #include "layer_norm.h"
 #include "sdden_internal.h"
+#include "sdden_rows.h"
+#include "time_table.h"
 
 namespace {
 
@@ -258,3 +263,135 @@ int sdden_gated_backward(int32_t R, int32_t d, int32_t H, int32_t act, const uin
 }
 
 }  // extern "C"
+
+// ------------------------------------------------------------------------------------------------ a denoiser of such layers
+// D(x, k) = h_L,  h_0 = x + e_k,  h_{l+1} = h_l + FF_l(LN_l(h_l)): the residual stream stays fp32, the block's rows are bf16.
+// Data flow per call: compaction of the unmasked rows; gather_add (h_0); per block the norm, the two first products with the
+// activation, and the last product, which adds the stream in place and in the last block scatters to the source rows.
+namespace {
+
+// h[m] = X[rowidx[m]] + table[krow[rowidx[m]]], 4 elements per thread and step
+__global__ __launch_bounds__(256) void gather_add_kernel(const float* __restrict__ X, const float* __restrict__ table,
+                                                         const int32_t* __restrict__ rowidx, const int32_t* __restrict__ krow,
+                                                         const int32_t* __restrict__ count, float* __restrict__ h, int d) {
+  const int per_row = d / 4;
+  const int64_t total = static_cast<int64_t>(*count) * per_row;
+  for (int64_t g = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x; g < total; g += static_cast<int64_t>(gridDim.x) * 256) {
+    const int m = static_cast<int>(g / per_row), c = static_cast<int>(g % per_row) * 4, src = rowidx[m];
+    const lgemm::f32x4 x = *reinterpret_cast<const lgemm::f32x4*>(X + static_cast<int64_t>(src) * d + c);
+    const lgemm::f32x4 e = *reinterpret_cast<const lgemm::f32x4*>(table + static_cast<int64_t>(krow[src]) * d + c);
+    *reinterpret_cast<lgemm::f32x4*>(h + static_cast<int64_t>(m) * d + c) = x + e;
+  }
+}
+
+struct GatedDenoiser final : sdden {
+  int H = 0, blocks = 0, act = 0, cap_rows = 0;
+  float eps = 0.f;
+  float *table = nullptr, *nw = nullptr, *nb = nullptr;              // [T,d], [blocks,d], [blocks,d]
+  uint16_t *Wg = nullptr, *Wu = nullptr, *Wd = nullptr;              // [blocks,H,d] x 2, [blocks,d,H]
+  int32_t *rowidx = nullptr, *count = nullptr;
+  float* h = nullptr;
+  uint16_t *n = nullptr, *hidden = nullptr;
+
+  ~GatedDenoiser() override {
+    for (void* q : {static_cast<void*>(table), static_cast<void*>(nw), static_cast<void*>(nb), static_cast<void*>(Wg),
+                    static_cast<void*>(Wu), static_cast<void*>(Wd), static_cast<void*>(rowidx), static_cast<void*>(count),
+                    static_cast<void*>(h), static_cast<void*>(n), static_cast<void*>(hidden)})
+      if (q) (void)hipFree(q);
+  }
+
+  int reserve(int R) override {
+    if (R <= cap_rows) return SD_OK;
+    for (void* q : {static_cast<void*>(rowidx), static_cast<void*>(h), static_cast<void*>(n), static_cast<void*>(hidden)})
+      if (q) (void)hipFree(q);
+    rowidx = nullptr; h = nullptr; n = hidden = nullptr; cap_rows = 0;
+    const size_t rows = static_cast<size_t>(R);
+    SD_HIP_TRY(err, hipMalloc(&rowidx, 4 * rows));
+    SD_HIP_TRY(err, hipMalloc(&h, 4 * rows * d));
+    SD_HIP_TRY(err, hipMalloc(&n, 2 * rows * d));
+    SD_HIP_TRY(err, hipMalloc(&hidden, 2 * rows * H));
+    if (!count) SD_HIP_TRY(err, hipMalloc(&count, 4));
+    cap_rows = R;
+    return SD_OK;
+  }
+
+  int eval(int R, const float* X, const int32_t* krow, float* out, hipStream_t st) override {
+    if (R > cap_rows)
+      return sdi::fail(err, SD_ERR_WORKSPACE, "sdden_eval(gated): %d rows exceed the %d reserved (sdden_reserve)", R, cap_rows);
+    if (!sdi::aligned16(X) || !sdi::aligned16(out))
+      return sdi::fail(err, SD_ERR_ARG, "sdden_eval(gated): X and out must be 16-byte aligned");
+    hipLaunchKernelGGL(sdrows::compact_rows_kernel, dim3(sdrows::compact_rows_grid(R)), dim3(sdrows::kScan), 0, st, krow, rowidx, count,
+                       active, rows_per_chain, R, T);
+    const int64_t chunks = static_cast<int64_t>(R) * (d / 4);
+    hipLaunchKernelGGL(gather_add_kernel, dim3(static_cast<unsigned>(std::min<int64_t>((chunks + 255) / 256, 256 * 32))), dim3(256), 0, st, X,
+                       table, rowidx, krow, count, h, d);
+    for (int l = 0; l < blocks; ++l) {
+      lnorm::Args a{};
+      a.R = R; a.d = d; a.x = h; a.ldx = d; a.y = n; a.ldy = d; a.eps = eps; a.count = count;
+      a.w = nw + static_cast<int64_t>(l) * d;
+      a.b = nb + static_cast<int64_t>(l) * d;
+      prof.mark(1, st);
+      by_type(4, SDDEN_F32, SDDEN_BF16, [&](auto v, auto tx, auto ty) { norm_forward<decltype(v)::value, decltype(tx), decltype(ty)>(a, st); });
+      prof.mark(1, st);
+      const int64_t wl = static_cast<int64_t>(l) * H * d;
+      lgemm::Args g{};
+      g.problems = 1;
+      g.act = act;
+      lgemm::Problem& p = g.p[0];
+      p.A[0] = n; p.lda = d; p.B[0] = Wg + wl; p.B[1] = Wu + wl; p.ldb = d; p.M = R; p.N = H; p.K = d; p.ranges = 1;
+      p.out = hidden; p.ldo = H; p.count = count;
+      prof.mark(2, st);
+      SD_HIP_TRY(err, (lgemm::launch<lgemm::kGate, lgemm::kAlong, lgemm::kAlong>(g, st)));
+      prof.mark(2, st);
+      p = lgemm::Problem{};
+      p.A[0] = hidden; p.lda = H; p.B[0] = Wd + wl; p.ldb = H; p.M = R; p.N = d; p.K = H; p.ranges = 1;
+      p.res = h; p.out_f32 = 1; p.ldo = d; p.count = count;
+      const bool last = l == blocks - 1;
+      p.out = last ? out : h;
+      p.rowidx = last ? rowidx : nullptr;
+      prof.mark(3, st);
+      SD_HIP_TRY(err, (lgemm::launch<lgemm::kStore, lgemm::kAlong, lgemm::kAlong>(g, st)));
+      prof.mark(3, st);
+    }
+    SD_HIP_TRY(err, hipGetLastError());
+    return SD_OK;
+  }
+};
+
+}  // namespace
+
+extern "C" int sdden_gated_create(int32_t d, int32_t H, int32_t E, int32_t blocks, int32_t act, const uint16_t* We, const float* be,
+                                  const float* norm_weight, const float* norm_bias, float eps, const uint16_t* Wg, const uint16_t* Wu,
+                                  const uint16_t* Wd, int32_t T, int32_t Rmax, sdden** out) try {
+  const char* what = "sdden_gated_create";
+  if ((E > 0 && !We) || !be || !norm_weight || !norm_bias || !Wg || !Wu || !Wd || !out || d <= 0 || H <= 0 || E < 0 || (E & 1) || blocks <= 0 ||
+      T <= 0 || Rmax <= 0 || (act != SDDEN_SILU && act != SDDEN_GELU) || !(eps >= 0.f) || std::isinf(eps))
+    return sdi::fail(LAYER_ERR, SD_ERR_ARG, "%s: bad argument", what);
+  if (d % 8 || H % 8 || d > kMaxStride || H > kMaxStride)
+    return sdi::fail(LAYER_ERR, SD_ERR_UNSUPPORTED, "%s: d=%d and H=%d must be multiples of 8 up to %lld", what, d, H,
+                     static_cast<long long>(kMaxStride));
+  std::unique_ptr<GatedDenoiser> m(new GatedDenoiser);
+  m->d = d; m->T = T; m->H = H; m->blocks = blocks; m->act = act; m->eps = eps;
+  const std::vector<float> table = sdtime::table(T, d, E, be, We);
+  hipError_t e = hipSuccess;
+  auto up = [&](auto** dst, const void* src, size_t bytes) {
+    if (e == hipSuccess) e = hipMalloc(reinterpret_cast<void**>(dst), bytes);
+    if (e == hipSuccess) e = hipMemcpy(*dst, src, bytes, hipMemcpyHostToDevice);
+  };
+  const size_t vec = static_cast<size_t>(blocks) * d * 4, mat = static_cast<size_t>(blocks) * d * H * 2;
+  up(&m->table, table.data(), table.size() * 4);
+  up(&m->nw, norm_weight, vec);
+  up(&m->nb, norm_bias, vec);
+  up(&m->Wg, Wg, mat);
+  up(&m->Wu, Wu, mat);
+  up(&m->Wd, Wd, mat);
+  if (e != hipSuccess) return sdi::fail(LAYER_ERR, SD_ERR_HIP, "%s: %s", what, hipGetErrorString(e));
+  if (int rc = m->reserve(Rmax)) {
+    LAYER_ERR = m->err;
+    return rc;
+  }
+  *out = m.release();
+  return SD_OK;
+} catch (const std::exception& ex) {
+  return sdi::fail(LAYER_ERR, SD_ERR_ARG, "sdden_gated_create: %s", ex.what());
+}

@@ -17,8 +17,6 @@
 // XCD-aware tile order) is in mlp_gemm.h.
 #include <hip/hip_runtime.h>
 
-#include <cmath>
-#include <cstring>
 #include <new>
 #include <vector>
 
@@ -27,6 +25,7 @@
 #include "mlp_gemm_pp.h"
 #include "sdden_internal.h"
 #include "sdden_rows.h"
+#include "time_table.h"
 
 namespace {
 
@@ -53,13 +52,6 @@ __global__ __launch_bounds__(kThreads) void gather_convert_kernel(const float* _
     o.w = to_bf16_bits(hi.z) | (static_cast<uint32_t>(to_bf16_bits(hi.w)) << 16);
     *reinterpret_cast<uint4*>(Xb + static_cast<int64_t>(m) * d + 8 * c) = o;
   }
-}
-
-float bf16_bits_to_float(uint16_t b) {
-  const uint32_t u = static_cast<uint32_t>(b) << 16;
-  float f;
-  std::memcpy(&f, &u, 4);
-  return f;
 }
 
 // Dynamic-LDS limits of every GEMM instantiation launch_gemm can pick, on the current device.
@@ -298,26 +290,8 @@ extern "C" int sdden_mlp_create(int32_t d, int32_t H, int32_t E, const uint16_t*
   MlpDenoiser* m = new (std::nothrow) MlpDenoiser;
   if (!m) return sdi::fail(ER, SD_ERR_ARG, "sdden_mlp_create: out of host memory");
   m->d = d; m->T = T; m->H = H; m->E = E;
-  // per-step bias table: tb[k] = b1 + emb(k) . W1[d:d+E, :],  emb = [sin(k w_i) ; cos(k w_i)], w_i = 10000^(-2i/E)
-  std::vector<float> tb(static_cast<size_t>(T) * H);
-  {
-    const int half = E / 2;
-    std::vector<double> emb(E > 0 ? E : 1), row(H);
-    for (int k = 0; k < T; ++k) {
-      for (int i = 0; i < half; ++i) {
-        const double w = std::pow(10000.0, -static_cast<double>(i) / half);
-        emb[i] = std::sin(k * w);
-        emb[half + i] = std::cos(k * w);
-      }
-      for (int n = 0; n < H; ++n) row[n] = b1[n];
-      for (int e = 0; e < E; ++e) {
-        const uint16_t* wrow = W1 + static_cast<size_t>(d + e) * H;
-        const double ev = emb[e];
-        for (int n = 0; n < H; ++n) row[n] += ev * bf16_bits_to_float(wrow[n]);
-      }
-      for (int n = 0; n < H; ++n) tb[static_cast<size_t>(k) * H + n] = static_cast<float>(row[n]);
-    }
-  }
+  // per-step bias table: b1 + emb(k) . W1[d:d+E, :]
+  const std::vector<float> tb = sdtime::table(T, H, E, b1, W1 + static_cast<size_t>(d) * H);
   std::vector<uint16_t> w1t, w2t, w3t;
   transpose_bits(W1, d, H, w1t);      // first d rows of W1 only: [d,H] -> [H,d]
   transpose_bits(W2, H, H, w2t);

@@ -1,10 +1,18 @@
 // Matrices kept in 4 bits with group scales (sdden_q4_*); kernels and layout in q4_product.h.
 #include <hip/hip_runtime.h>
 
+#include <algorithm>
+#include <cmath>
+#include <cstring>
+#include <exception>
+#include <memory>
 #include <new>
+#include <vector>
 
 #include "q4_matrix.h"
 #include "sdden_internal.h"
+#include "sdden_rows.h"
+#include "time_table.h"
 
 #define Q4_ERR sdi::g_den_create_error
 
@@ -60,3 +68,159 @@ int sdden_q4_destroy(sdden_q4* m) {
 }
 
 }  // extern "C"
+
+// ------------------------------------------------------------------------------------------------ the MLP denoiser in 4 bits
+// The network of sdden_mlp.hip with its three matrices in 4 bits, as a draft model that reads a quarter of the target's bytes:
+//   compact_rows     unmasked rows -> dense list
+//   product 1        H1 = silu(X Q1 + tb[krow])    rows gathered, rounded to bf16 as they enter (or the caller's bf16 image)
+//   product 2        H2 = silu(H1 Q2 + b2)
+//   product 3        out[rowidx] = H2 Q3 + b3       fp32
+namespace {
+
+float bf16_round(float x) {          // to nearest even; finite values only
+  uint32_t u;
+  std::memcpy(&u, &x, 4);
+  u = (u + 0x7FFFu + ((u >> 16) & 1u)) & 0xFFFF0000u;
+  std::memcpy(&x, &u, 4);
+  return x;
+}
+
+// W [K, N] bf16 (row = input) -> q [N, ceil(K/2)], scale [N, ceil(K/group)]: scale = bf16(max |w| / 7) over the group's inputs,
+// q = round(w / scale) + 8 within 0..15; a group of zeros has scale 0 and q = 8.
+void quantize(const uint16_t* W, int K, int N, int group, std::vector<uint8_t>& q, std::vector<uint16_t>& scale) {
+  const int groups = (K + group - 1) / group;
+  const size_t rowbytes = (static_cast<size_t>(K) + 1) / 2;
+  q.assign(static_cast<size_t>(N) * rowbytes, 0);
+  scale.assign(static_cast<size_t>(N) * groups, 0);
+  constexpr int NB = 64;              // columns at a time: a row's 128 bytes are read together
+  for (int n0 = 0; n0 < N; n0 += NB) {
+    const int nb = std::min(NB, N - n0);
+    for (int g = 0; g < groups; ++g) {
+      const int k0 = g * group, k1 = std::min(K, k0 + group);
+      float amax[NB] = {}, s[NB];
+      for (int k = k0; k < k1; ++k)
+        for (int i = 0; i < nb; ++i) amax[i] = std::max(amax[i], std::fabs(sdtime::bf16_bits_to_float(W[static_cast<size_t>(k) * N + n0 + i])));
+      for (int i = 0; i < nb; ++i) {
+        s[i] = bf16_round(amax[i] / 7.0f);
+        uint32_t u;
+        std::memcpy(&u, &s[i], 4);
+        scale[static_cast<size_t>(n0 + i) * groups + g] = static_cast<uint16_t>(u >> 16);
+      }
+      for (int k = k0; k < k1; ++k)
+        for (int i = 0; i < nb; ++i) {
+          const float w = sdtime::bf16_bits_to_float(W[static_cast<size_t>(k) * N + n0 + i]);
+          const float v = s[i] > 0.f ? std::nearbyint(w / s[i]) : 0.f;
+          const int c = static_cast<int>(std::min(7.f, std::max(-8.f, v))) + 8;
+          q[(n0 + i) * rowbytes + (k >> 1)] |= static_cast<uint8_t>(k & 1 ? c << 4 : c);
+        }
+    }
+  }
+}
+
+struct Mlp4Denoiser final : sdden {
+  int H = 0, cap_rows = 0;
+  sdden_q4 Q1, Q2, Q3;
+  float *tb = nullptr, *b2 = nullptr, *b3 = nullptr;      // [T,H], [H], [d]
+  int32_t *rowidx = nullptr, *count = nullptr;
+  uint16_t *H1 = nullptr, *H2 = nullptr;
+  int64_t ldh = 0;                                        // rows of H1 and H2 start on 16 bytes
+
+  ~Mlp4Denoiser() override {
+    for (void* p : {static_cast<void*>(tb), static_cast<void*>(b2), static_cast<void*>(b3), static_cast<void*>(rowidx),
+                    static_cast<void*>(count), static_cast<void*>(H1), static_cast<void*>(H2)})
+      if (p) (void)hipFree(p);
+  }
+
+  int reserve(int R) override {
+    if (R <= cap_rows) return SD_OK;
+    for (void* p : {static_cast<void*>(rowidx), static_cast<void*>(H1), static_cast<void*>(H2)})
+      if (p) (void)hipFree(p);
+    rowidx = nullptr; H1 = H2 = nullptr; cap_rows = 0;
+    ldh = (H + 7) / 8 * 8;
+    SD_HIP_TRY(err, hipMalloc(&rowidx, 4 * static_cast<size_t>(R)));
+    SD_HIP_TRY(err, hipMalloc(&H1, 2 * static_cast<size_t>(R) * ldh));
+    SD_HIP_TRY(err, hipMalloc(&H2, 2 * static_cast<size_t>(R) * ldh));
+    if (!count) SD_HIP_TRY(err, hipMalloc(&count, 4));
+    cap_rows = R;
+    return SD_OK;
+  }
+
+  int eval(int R, const float* X, const int32_t* krow, float* out, hipStream_t st) override { return go(R, X, nullptr, krow, out, st); }
+  int eval_mirror(int R, const float* X, const uint16_t* Xb, const int32_t* krow, float* out, hipStream_t st) override {
+    return go(R, X, Xb, krow, out, st);
+  }
+
+  int go(int R, const float* X, const uint16_t* Xb, const int32_t* krow, float* out, hipStream_t st) {
+    if (R > cap_rows)
+      return sdi::fail(err, SD_ERR_WORKSPACE, "sdden_eval(mlp4): %d rows exceed the %d reserved (sdden_reserve)", R, cap_rows);
+    if (!sdi::aligned16(X) || !sdi::aligned16(out) || !sdi::aligned16(Xb))
+      return sdi::fail(err, SD_ERR_ARG, "sdden_eval(mlp4): X, its image and out must be 16-byte aligned");
+    hipLaunchKernelGGL(sdrows::compact_rows_kernel, dim3(sdrows::compact_rows_grid(R)), dim3(sdrows::kScan), 0, st, krow, rowidx, count,
+                       active, rows_per_chain, R, T);
+    q4::Args a{};
+    Q1.fill(a);
+    a.X = Xb ? static_cast<const void*>(Xb) : X; a.ldx = d; a.R = R; a.vec = d % (Xb ? 8 : 4) == 0;
+    a.bias = tb; a.krow = krow; a.rowidx = rowidx; a.count = count; a.gather = true; a.silu = true;
+    a.Y = H1; a.ldy = ldh; a.vec_out = true;
+    prof.mark(1, st);
+    SD_HIP_TRY(err, Q1.launch(a, R, Xb ? q4::kBf16 : q4::kF32Rounded, st));
+    prof.mark(1, st);
+    a = q4::Args{};
+    Q2.fill(a);
+    a.X = H1; a.ldx = ldh; a.R = R; a.vec = true; a.bias = b2; a.count = count; a.silu = true; a.Y = H2; a.ldy = ldh; a.vec_out = true;
+    prof.mark(2, st);
+    SD_HIP_TRY(err, Q2.launch(a, R, q4::kBf16, st));
+    prof.mark(2, st);
+    a = q4::Args{};
+    Q3.fill(a);
+    a.X = H2; a.ldx = ldh; a.R = R; a.vec = true; a.bias = b3; a.count = count; a.rowidx = rowidx; a.scatter = true;
+    a.Y = out; a.ldy = d; a.y_f32 = true; a.vec_out = d % 4 == 0;
+    prof.mark(3, st);
+    SD_HIP_TRY(err, Q3.launch(a, R, q4::kBf16, st));
+    prof.mark(3, st);
+    SD_HIP_TRY(err, hipGetLastError());
+    return SD_OK;
+  }
+};
+
+}  // namespace
+
+extern "C" int sdden_mlp4_create(int32_t d, int32_t H, int32_t E, int32_t group, const uint16_t* W1, const float* b1, const uint16_t* W2,
+                                 const float* b2, const uint16_t* W3, const float* b3, int32_t T, int32_t Rmax, sdden** out) try {
+  const char* what = "sdden_mlp4_create";
+  if (!W1 || !b1 || !W2 || !b2 || !W3 || !b3 || !out || d <= 0 || H <= 0 || E < 0 || (E & 1) || T <= 0 || Rmax <= 0)
+    return sdi::fail(Q4_ERR, SD_ERR_ARG, "%s: bad argument", what);
+  if ((group != 32 && group != 64 && (group <= 0 || group % 128)) || d > q4::kMaxDim || H > q4::kMaxDim)
+    return sdi::fail(Q4_ERR, SD_ERR_UNSUPPORTED, "%s: group=%d must be 32, 64 or a multiple of 128, d=%d and H=%d at most %d", what, group, d, H,
+                     q4::kMaxDim);
+  std::unique_ptr<Mlp4Denoiser> m(new Mlp4Denoiser);
+  m->d = d; m->T = T; m->H = H;
+  const std::vector<float> tb = sdtime::table(T, H, E, b1, W1 + static_cast<size_t>(d) * H);
+  hipError_t e = hipSuccess;
+  std::vector<uint8_t> q;
+  std::vector<uint16_t> s;
+  auto matrix = [&](sdden_q4& M, const uint16_t* W, int K, int N) {
+    if (e != hipSuccess) return;
+    quantize(W, K, N, group, q, s);
+    e = M.upload(N, K, group, q.data(), s.data());
+  };
+  auto up = [&](float** dst, const float* src, size_t n) {
+    if (e == hipSuccess) e = hipMalloc(reinterpret_cast<void**>(dst), 4 * n);
+    if (e == hipSuccess) e = hipMemcpy(*dst, src, 4 * n, hipMemcpyHostToDevice);
+  };
+  up(&m->tb, tb.data(), tb.size());
+  up(&m->b2, b2, H);
+  up(&m->b3, b3, d);
+  matrix(m->Q1, W1, d, H);
+  matrix(m->Q2, W2, H, H);
+  matrix(m->Q3, W3, H, d);
+  if (e != hipSuccess) return sdi::fail(Q4_ERR, SD_ERR_HIP, "%s: %s", what, hipGetErrorString(e));
+  if (int rc = m->reserve(Rmax)) {
+    Q4_ERR = m->err;
+    return rc;
+  }
+  *out = m.release();
+  return SD_OK;
+} catch (const std::exception& ex) {
+  return sdi::fail(Q4_ERR, SD_ERR_ARG, "sdden_mlp4_create: %s", ex.what());
+}

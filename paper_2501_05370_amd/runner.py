@@ -3,6 +3,8 @@ from __future__ import annotations
 
 import torch
 
+from workloads import GatedParams, Q4MLPParams
+
 from .binding import Context, Denoiser
 from .sampler import DiffusionSampler, EfficientFrozenSampler, IndependentDrafterSampler, LangevinSampler, Phi4LangevinSampler
 
@@ -15,7 +17,13 @@ def make_context(cfg, seed=None) -> Context:
 
 
 def make_denoiser(cfg, max_rows: int, params=None) -> Denoiser:
+    """The denoiser of ``cfg``'s parameters, or of ``params``: of the workload's kind, or one of the networks that have a type of
+    their own (4-bit and gated ones), which serve as target or draft of any diffusion workload."""
     p, s = (cfg.params if params is None else params), cfg.schedule
+    if isinstance(p, Q4MLPParams):
+        return Denoiser.sdden_mlp4_create(p.p, p.group, cfg.T, max_rows)
+    if isinstance(p, GatedParams):
+        return Denoiser.sdden_gated_create(p, cfg.T, max_rows)
     if cfg.kind == "gmm":
         return Denoiser.sdden_gmm_create(p.means, p.stds, p.logw, s.alpha_bar_state)
     if cfg.kind == "lowrank":

@@ -113,3 +113,49 @@ def test_q4_binding_checks_shapes():
                 dict(q=q, scale=s.astype(np.float32), K=65, group=32), dict(q=q, scale=s, K=65, group=0), dict(q=q[0], scale=s, K=65, group=32)):
         with pytest.raises(B.SDError, match="sdden_q4_create"):
             B.Q4Matrix.sdden_q4_create(**bad)
+
+
+def _ptrs(n):
+    import numpy as np
+    a = np.zeros(64 * 64, np.uint16)
+    f = np.zeros(64 * 64, np.float32)
+    return a, f
+
+
+@pytest.mark.parametrize("kw,rc", [(dict(d=0), -1), (dict(H=-1), -1), (dict(E=3), -1), (dict(T=0), -1), (dict(Rmax=0), -1), (dict(group=48), -5),
+                                   (dict(group=0), -5), (dict(d=(1 << 20) + 1), -5), (dict(null=True), -1)])
+def test_mlp4_create_refuses(kw, rc):
+    a, f = _ptrs(1)
+    v = dict(d=8, H=8, E=2, group=32, T=4, Rmax=4, null=False)
+    v.update(kw)
+    h = ctypes.c_void_p()
+    w = None if v["null"] else a.ctypes.data
+    assert B.load_library().sdden_mlp4_create(v["d"], v["H"], v["E"], v["group"], w, f.ctypes.data, a.ctypes.data, f.ctypes.data,
+                                              a.ctypes.data, f.ctypes.data, v["T"], v["Rmax"], ctypes.byref(h)) == rc
+    assert "sdden_mlp4_create" in err()
+
+
+@pytest.mark.parametrize("kw,rc", [(dict(d=12), -5), (dict(H=20), -5), (dict(E=1), -1), (dict(blocks=0), -1), (dict(act=2), -1),
+                                   (dict(eps=float("nan")), -1), (dict(T=0), -1), (dict(Rmax=-1), -1), (dict(null=True), -1)])
+def test_gated_create_refuses(kw, rc):
+    a, f = _ptrs(1)
+    v = dict(d=8, H=8, E=2, blocks=1, act=0, eps=1e-5, T=4, Rmax=4, null=False)
+    v.update(kw)
+    h = ctypes.c_void_p()
+    w = None if v["null"] else a.ctypes.data
+    assert B.load_library().sdden_gated_create(v["d"], v["H"], v["E"], v["blocks"], v["act"], a.ctypes.data, f.ctypes.data, f.ctypes.data,
+                                               f.ctypes.data, v["eps"], w, a.ctypes.data, a.ctypes.data, v["T"], v["Rmax"], ctypes.byref(h)) == rc
+    assert "sdden_gated_create" in err()
+
+
+def test_network_bindings_check_shapes():
+    import numpy as np
+    import workloads as W
+    p = W.random_mlp(np.random.default_rng(0), 8, 8, 2)
+    p.W2 = p.W2[:4]
+    with pytest.raises(B.SDError, match="mlp4"):
+        B.Denoiser.sdden_mlp4_create(p, 32, 4, 4)
+    g = W.random_gated(np.random.default_rng(0), 8, 16, 2, 2)
+    g.norm_bias = g.norm_bias[:1]
+    with pytest.raises(B.SDError, match="gated"):
+        B.Denoiser.sdden_gated_create(g, 4, 4)

@@ -133,6 +133,30 @@ class MLPParams:
     b3: np.ndarray
 
 
+@dataclass
+class Q4MLPParams:
+    """The same network with its matrices in 4 bits (the library quantises them): a draft model of ``p``."""
+    p: MLPParams
+    group: int                          # inputs per scale: 32, 64 or a multiple of 128
+
+
+@dataclass
+class GatedParams:
+    """x0-predicting residual network: h0 = x + be + temb(k) We, then h += (f(n Wg^T) * (n Wu^T)) Wd^T with n = LN(h) per block."""
+    d: int
+    H: int
+    E: int
+    act: int                            # 0 SiLU, 1 GELU
+    eps: float
+    We: np.ndarray                      # uint16 [E, d]          bf16 bits
+    be: np.ndarray                      # fp32-valued [d]
+    norm_weight: np.ndarray             # fp32-valued [blocks, d]
+    norm_bias: np.ndarray
+    Wg: np.ndarray                      # uint16 [blocks, H, d]  row = output feature
+    Wu: np.ndarray
+    Wd: np.ndarray                      # uint16 [blocks, d, H]
+
+
 def bf16_round_bits(x: np.ndarray) -> np.ndarray:
     """fp32 -> bf16 bit pattern (uint16), round-to-nearest-even. Data preparation only."""
     u = np.ascontiguousarray(x, dtype=np.float32).view(np.uint32)
@@ -181,6 +205,16 @@ def random_mlp(rng: np.random.Generator, d: int, H: int, E: int = 256) -> MLPPar
     W2, b2 = layer(H, H)
     W3, b3 = layer(H, d)
     return MLPParams(d, H, E, W1, b1, W2, b2, W3, b3)
+
+
+def random_gated(rng: np.random.Generator, d: int, H: int, blocks: int, E: int = 256, act: int = 0) -> GatedParams:
+    """Normal weights of std 1/sqrt(fan_in), the last products' scaled down by sqrt(2 blocks) so that the stream keeps its size."""
+    def mat(*shape, std):
+        return bf16_round_bits(rng.standard_normal(shape, dtype=np.float32) * np.float32(std))
+    return GatedParams(d, H, E, act, 1e-5, mat(E, d, std=1.0 / np.sqrt(max(1, E))), _f32(rng.uniform(-0.1, 0.1, size=d)),
+                       _f32(1.0 + 0.2 * rng.standard_normal((blocks, d))), _f32(0.1 * rng.standard_normal((blocks, d))),
+                       mat(blocks, H, d, std=d ** -0.5), mat(blocks, H, d, std=d ** -0.5),
+                       mat(blocks, d, H, std=(H * 2.0 * blocks) ** -0.5))
 
 
 # --------------------------------------------------------------------------------------
