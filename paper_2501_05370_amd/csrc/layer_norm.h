@@ -56,18 +56,7 @@ __device__ __forceinline__ void store(T* p, const float (&v)[V]) {
   }
 }
 
-template <int MASK>
-__device__ __forceinline__ float xor_add(float v) {
-  return v + __int_as_float(sdlane::lane_xor<MASK>(__float_as_int(v)));
-}
-__device__ __forceinline__ float wave_sum(float v) {
-  v = xor_add<1>(v);
-  v = xor_add<2>(v);
-  v = xor_add<4>(v);
-  v = xor_add<8>(v);
-  v = xor_add<16>(v);
-  return xor_add<32>(v);
-}
+using sdlane::wave_sum;
 
 // Sums of a and b over the TPR threads of a row; `slot` alternates between calls so that one barrier per call is enough.
 template <int TPR>

@@ -6,8 +6,9 @@
 //   unpacking   a byte 0 .. 15 read as an 8-bit float (e4m3) is q 2^-9: the subnormals and the first binade are one linear
 //               scale.  The hardware's conversion of two such bytes to two bf16 with a scale of 2^9 gives q exactly: 7
 //               instructions per 8 weights (two masks, a shift, four conversions)
-//   the -8      the sum of a group starts from -8 sum(x), which a matrix instruction with a constant operand leaves in just the
-//               layout of the sum; one such chain serves every 16 columns a wavefront computes on the same rows
+//   the -8      the sum of a group starts from -8 sum(x), which matrix instructions with a constant operand leave in just the
+//               layout of the sum; one such chain serves all the columns a wavefront computes on the same rows.  (Summed by the
+//               vector units as the rows are written to LDS, 512 rows x 4096 x 12288 take 92 us instead of 81: those bound the call.)
 //   fp32 rows   are three bf16 pieces (8 + 8 + 8 bits: exact) that take three rows of the tile; the epilogue adds them up
 // The order of a sum is the same everywhere: within a group along k, the groups of the blocks b = i, i + 8, i + 16, ... (128 k
 // each) in that order for i = 0 .. 7, and then those eight sums; so a row's result does not depend on the call it is part of.
@@ -34,7 +35,7 @@ using lgemm::u32x2;
 using lgemm::u32x4;
 typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 
-// How rows enter: as they are, fp32 exactly (three pieces), fp32 rounded to bf16 first.
+// How rows enter: as they are, fp32 exactly (three pieces), fp32 rounded to bf16 first (a denoiser's call of up to 32 rows).
 enum Rows { kBf16 = 0, kF32 = 1, kF32Rounded = 2 };
 __host__ __device__ constexpr int pieces(int rows) { return rows == kF32 ? 3 : 1; }
 
@@ -73,34 +74,64 @@ __device__ __forceinline__ f32x4 add_scaled(f32x4 a, f32x4 s, f32x4 c) {
   return a;
 }
 
+__device__ __forceinline__ bf16x8 minus8() {
+  bf16x8 v;
+#pragma unroll
+  for (int e = 0; e < 8; ++e) v[e] = static_cast<__bf16>(-8.f);
+  return v;
+}
+
 constexpr int kShares = 8;       // partial sums of an output, see the top
+constexpr int kManyRows = 64;    // tile rows of many_kernel
 
 // Eight values of a row from k on; past K they are 0.
-template <int ROWS>
-struct Chunk {
-  typedef typename std::conditional<ROWS == kBf16, bf16x8, f32x4[2]>::type Raw;
+struct F32x8 {
+  f32x4 v[2];
+  __device__ __forceinline__ f32x4& operator[](int i) { return v[i]; }
+  __device__ __forceinline__ const f32x4& operator[](int i) const { return v[i]; }
 };
 
 template <int ROWS>
+struct Chunk {
+  typedef typename std::conditional<ROWS == kBf16, bf16x8, F32x8>::type Raw;
+};
+
+// VEC: rows start on 16 bytes and K is a multiple of 8, so a chunk lies wholly before K or behind it: it is loaded without a branch
+// (from the row's last chunk where it lies behind) and zeroed when it is used.
+template <int ROWS, bool VEC>
 __device__ __forceinline__ void load_chunk(const Args& p, int64_t src, int k, typename Chunk<ROWS>::Raw& v) {
-  if constexpr (ROWS == kBf16) {
-    const __bf16* x = static_cast<const __bf16*>(p.X) + src * p.ldx + k;
-    if (p.vec && k + 8 <= p.K) {
+  typedef typename std::conditional<ROWS == kBf16, __bf16, float>::type T;
+  const T* x = static_cast<const T*>(p.X) + src * p.ldx;
+  if constexpr (VEC) {
+    x += k < p.K ? k : p.K - 8;
+    if constexpr (ROWS == kBf16) {
       v = *reinterpret_cast<const bf16x8*>(x);
     } else {
-#pragma unroll
-      for (int e = 0; e < 8; ++e) v[e] = k + e < p.K ? x[e] : static_cast<__bf16>(0.f);
-    }
-  } else {
-    const float* x = static_cast<const float*>(p.X) + src * p.ldx + k;
-    if (p.vec && k + 8 <= p.K) {
       v[0] = *reinterpret_cast<const f32x4*>(x);
       v[1] = *reinterpret_cast<const f32x4*>(x + 4);
-    } else {
+    }
+  } else {
 #pragma unroll
-      for (int e = 0; e < 8; ++e) v[e >> 2][e & 3] = k + e < p.K ? x[e] : 0.f;
+    for (int e = 0; e < 8; ++e) {
+      const T t = k + e < p.K ? x[k + e] : static_cast<T>(0.f);
+      if constexpr (ROWS == kBf16) v[e] = t;
+      else v[e >> 2][e & 3] = t;
     }
   }
+}
+
+template <int ROWS>
+__device__ __forceinline__ typename Chunk<ROWS>::Raw zero_if(bool behind, typename Chunk<ROWS>::Raw v) {
+  if constexpr (ROWS == kBf16) {
+    u32x4 t = __builtin_bit_cast(u32x4, v);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) t[e] = behind ? 0u : t[e];
+    v = __builtin_bit_cast(bf16x8, t);
+  } else {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v.v[e >> 2][e & 3] = behind ? 0.f : v.v[e >> 2][e & 3];
+  }
+  return v;
 }
 
 // A row of 128 k is 256 bytes of LDS, all 64 banks: chunk c (8 k) of row v lies at c ^ (v & 15), so that a fragment read (16 rows,
@@ -124,12 +155,11 @@ __device__ __forceinline__ void put_chunk(unsigned char* panel, int row, int c, 
         lo[e] = static_cast<__bf16>(r - static_cast<float>(mid[e]));
       }
     }
+    const int first = ROWS == kF32 ? 3 * row : row;
+    *reinterpret_cast<bf16x8*>(panel + lds_chunk(first, c)) = hi;
     if constexpr (ROWS == kF32) {
-      *reinterpret_cast<bf16x8*>(panel + lds_chunk(3 * row, c)) = hi;
-      *reinterpret_cast<bf16x8*>(panel + lds_chunk(3 * row + 1, c)) = mid;
-      *reinterpret_cast<bf16x8*>(panel + lds_chunk(3 * row + 2, c)) = lo;
-    } else {
-      *reinterpret_cast<bf16x8*>(panel + lds_chunk(row, c)) = hi;
+      *reinterpret_cast<bf16x8*>(panel + lds_chunk(first + 1, c)) = mid;
+      *reinterpret_cast<bf16x8*>(panel + lds_chunk(first + 2, c)) = lo;
     }
   }
 }
@@ -173,268 +203,293 @@ __device__ __forceinline__ void finish4(const Args& p, int m, int n, f32x4 c) {
   }
 }
 
-constexpr float kMinus8 = -8.f;
-__device__ __forceinline__ bf16x8 minus8() {
-  bf16x8 v;
-#pragma unroll
-  for (int e = 0; e < 8; ++e) v[e] = static_cast<__bf16>(kMinus8);
-  return v;
-}
-
 // ------------------------------------------------------------------------------------------------ few rows
-// A workgroup computes 16 columns of up to 16 MT tile rows; its eight wavefronts take the blocks of 128 k in turn (together they
+// A workgroup computes 16 NT columns of up to 16 MT tile rows; its eight wavefronts take the blocks of 128 k in turn (together they
 // stream the columns' blocks as they lie), each with its own panel of rows in LDS, and their sums meet in LDS at the end, in order.
-// Weights are requested two blocks ahead, rows one, in registers: there is no barrier in the loop.
-template <int MT, int GPB, int ROWS>
-__global__ __launch_bounds__(512) void few_kernel(Args p) {
-  constexpr int NW = kShares, kPanel = 16 * MT * 256, PIECES = pieces(ROWS), kRealRows = 16 * MT / PIECES;
-  constexpr int kChunks = (kRealRows * 16 + 63) / 64;       // chunks of a block per lane
+// Weights and rows (XC chunks of 8 per lane: 4 XC rows) are requested PF blocks ahead in registers, PF being what these hold: both alike, as loads
+// return in order and waiting for a row would wait for every weight requested before it.  There is no barrier in the loop.  Tile rows
+// that no row of the call fills hold whatever was there: their sums are not used.
+template <int MT, int NT, int GPB, int ROWS, int XC, int PF, bool VEC>
+__global__ __launch_bounds__(64 * kShares) void few_kernel(Args p) {
+  constexpr int NW = kShares, PIECES = pieces(ROWS), kRealRows = 16 * MT / PIECES, kChunks = XC;
+  constexpr int kPanel = 16 * MT * 256;
+  static_assert(4 * XC <= kRealRows + 3, "rows");
+  static_assert(MT * NT * 16 * 64 <= kPanel, "the sums take the panels' place");
   __shared__ __align__(1024) unsigned char lds[NW * kPanel];
   const int t = threadIdx.x, lane = t & 63, wave = __builtin_amdgcn_readfirstlane(t >> 6), l16 = lane & 15, lq = lane >> 4;
-  // the row groups of a tile run on the same XCD, one after the other: its L2 serves the weights to all but the first
-  const int groups = gridDim.x / ((p.ntiles + 7) / 8 * 8), id = blockIdx.x >> 3;
-  const int tile = (id / groups) * 8 + (blockIdx.x & 7), group = id % groups;
-  if (tile >= p.ntiles) return;
-  const int M = p.count ? *p.count : p.R;
-  const int row0 = group * kRealRows, rows = M - row0 < kRealRows ? M - row0 : kRealRows;
+  const int tile0 = blockIdx.x * NT;
+  const int row0 = blockIdx.y * kRealRows, M = (p.count ? (*p.count < p.R ? *p.count : p.R) : p.R) - row0;
+  const int rows = M < kRealRows ? M : kRealRows;
   if (rows <= 0) return;
   unsigned char* panel = lds + wave * kPanel;
-  for (int i = lane; i < kPanel / 16; i += 64) *reinterpret_cast<u32x4*>(panel + 16 * i) = u32x4{0, 0, 0, 0};
+  const bf16x8 m8 = minus8();
 
+  const u32x4* W[NT];
+  const uint16_t* S[NT];
+#pragma unroll
+  for (int n = 0; n < NT; ++n) {
+    const int64_t tile = tile0 + n < p.ntiles ? tile0 + n : p.ntiles - 1;
+    W[n] = p.W + tile * p.kblocks * 64 + lane;
+    S[n] = p.S + tile * p.kblocks * GPB * 16 + 4 * lq;
+  }
+  u32x4 w[PF][NT];
+  u32x2 s[PF][NT][GPB];
+  // what lies past the last block is requested again instead: no branch between the loads, which the compiler could only wait out
+  auto fetch_weights = [&](int b, u32x4 (&w)[NT], u32x2 (&s)[NT][GPB]) {
+    b = b < p.kblocks ? b : p.kblocks - 1;
+#pragma unroll
+    for (int n = 0; n < NT; ++n) {
+      w[n] = W[n][static_cast<int64_t>(b) * 64];
+#pragma unroll
+      for (int g = 0; g < GPB; ++g) s[n][g] = *reinterpret_cast<const u32x2*>(S[n] + (static_cast<int64_t>(b) * GPB + g) * 16);
+    }
+  };
   int src[kChunks];
 #pragma unroll
   for (int i = 0; i < kChunks; ++i) {
-    const int r = (64 * i + lane) >> 4;
-    src[i] = r < rows ? (p.gather ? p.rowidx[row0 + r] : row0 + r) : -1;
+    const int r = (64 * i + lane) >> 4, row = r < rows ? r : rows - 1;
+    src[i] = p.gather ? p.rowidx[row0 + row] : row0 + row;
   }
   typedef typename Chunk<ROWS>::Raw Raw;
-  Raw x[kChunks];
-  auto fetch_rows = [&](int b) {
+  Raw x[PF][kChunks];
+  auto fetch_rows = [&](int b, Raw (&x)[kChunks]) {
+    if (!VEC && b >= p.kblocks) return;          // element by element, a repetition would cost
+    b = b < p.kblocks ? b : p.kblocks - 1;
 #pragma unroll
-    for (int i = 0; i < kChunks; ++i)
-      if (src[i] >= 0) load_chunk<ROWS>(p, src[i], 128 * b + 8 * l16, x[i]);
+    for (int i = 0; i < kChunks; ++i) load_chunk<ROWS, VEC>(p, src[i], 128 * b + 8 * l16, x[i]);
   };
-  const u32x4* W = p.W + (static_cast<int64_t>(tile) * p.kblocks) * 64 + lane;
-  const uint16_t* S = p.S + static_cast<int64_t>(tile) * p.kblocks * GPB * 16 + 4 * lq;
-  u32x4 w0{}, w1{}, w2{};
-  u32x2 s0[GPB] = {}, s1[GPB] = {}, s2[GPB] = {};
-  auto fetch_weights = [&](int b, u32x4& w, u32x2 (&s)[GPB]) {
-    if (b < p.kblocks) {
-      w = W[static_cast<int64_t>(b) * 64];
 #pragma unroll
-      for (int g = 0; g < GPB; ++g) s[g] = *reinterpret_cast<const u32x2*>(S + (static_cast<int64_t>(b) * GPB + g) * 16);
-    }
-  };
-  f32x4 acc[MT];
+  for (int i = 0; i < PF; ++i) {
+    fetch_weights(wave + i * NW, w[i], s[i]);
+    fetch_rows(wave + i * NW, x[i]);
+  }
+  f32x4 acc[MT][NT] = {};
+  for (int b0 = wave; b0 < p.kblocks; b0 += PF * NW) {
 #pragma unroll
-  for (int i = 0; i < MT; ++i) acc[i] = f32x4{0.f, 0.f, 0.f, 0.f};
-  int b = wave;
-  fetch_weights(b, w0, s0);
-  fetch_weights(b + NW, w1, s1);
-  if (b < p.kblocks) fetch_rows(b);
-  const bf16x8 m8 = minus8();
-  for (; b < p.kblocks; b += NW) {
-    fetch_weights(b + 2 * NW, w2, s2);
+    for (int i = 0; i < PF; ++i) {
+      const int b = b0 + i * NW;
+      if (b >= p.kblocks) break;
 #pragma unroll
-    for (int i = 0; i < kChunks; ++i)
-      if (src[i] >= 0) put_chunk<ROWS>(panel, (64 * i + lane) >> 4, l16, x[i]);
-    if (b + NW < p.kblocks) fetch_rows(b + NW);
-    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-    __builtin_amdgcn_wave_barrier();
+      for (int c = 0; c < kChunks; ++c)
+        if (4 * XC <= kRealRows || (64 * c + lane) >> 4 < kRealRows)
+          put_chunk<ROWS>(panel, (64 * c + lane) >> 4, l16, VEC && 128 * b + 128 > p.K ? zero_if<ROWS>(128 * b + 8 * l16 >= p.K, x[i][c]) : x[i][c]);
+      fetch_rows(b + PF * NW, x[i]);
+      __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+      __builtin_amdgcn_wave_barrier();
 #pragma unroll
-    for (int g = 0; g < GPB; ++g) {
-      constexpr int J = 4 / GPB;
-      bf16x8 wf[J];
+      for (int g = 0; g < GPB; ++g) {
+        constexpr int J = 4 / GPB;
+        bf16x8 xf[MT][J];
+        f32x4 c[MT][NT];
 #pragma unroll
-      for (int j = 0; j < J; ++j) wf[j] = unpack(w0[g * J + j]);
-      const f32x4 s = scales4(s0[g]);
+        for (int j = 0; j < J; ++j)
 #pragma unroll
-      for (int i = 0; i < MT; ++i) {
-        bf16x8 xf[J];
-        f32x4 c{0.f, 0.f, 0.f, 0.f};
+          for (int m = 0; m < MT; ++m) {
+            xf[m][j] = get_fragment(panel, 16 * m, g * J + j, l16, lq);
+            c[m][0] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(m8, xf[m][j], j ? c[m][0] : f32x4{0.f, 0.f, 0.f, 0.f}, 0, 0, 0);
+          }
 #pragma unroll
-        for (int j = 0; j < J; ++j) xf[j] = get_fragment(panel, 16 * i, g * J + j, l16, lq);
+        for (int m = 0; m < MT; ++m)
 #pragma unroll
-        for (int j = 0; j < J; ++j) c = __builtin_amdgcn_mfma_f32_16x16x32_bf16(m8, xf[j], c, 0, 0, 0);
+          for (int n = 1; n < NT; ++n) c[m][n] = c[m][0];
 #pragma unroll
-        for (int j = 0; j < J; ++j) c = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wf[j], xf[j], c, 0, 0, 0);
-        acc[i] = add_scaled(acc[i], s, c);
+        for (int j = 0; j < J; ++j) {
+          bf16x8 wf[NT];
+#pragma unroll
+          for (int n = 0; n < NT; ++n) wf[n] = unpack(w[i][n][g * J + j]);
+#pragma unroll
+          for (int m = 0; m < MT; ++m)
+#pragma unroll
+            for (int n = 0; n < NT; ++n) c[m][n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wf[n], xf[m][j], c[m][n], 0, 0, 0);
+        }
+#pragma unroll
+        for (int n = 0; n < NT; ++n) {
+          const f32x4 sc = scales4(s[i][n][g]);
+#pragma unroll
+          for (int m = 0; m < MT; ++m) acc[m][n] = add_scaled(acc[m][n], sc, c[m][n]);
+        }
+        if (GPB > 1) __builtin_amdgcn_sched_barrier(0);     // the groups one after the other: registers
       }
-    }
-    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-    __builtin_amdgcn_wave_barrier();
-    w0 = w1;
-    w1 = w2;
-#pragma unroll
-    for (int g = 0; g < GPB; ++g) {
-      s0[g] = s1[g];
-      s1[g] = s2[g];
+      fetch_weights(b + PF * NW, w[i], s[i]);
+      __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+      __builtin_amdgcn_wave_barrier();
     }
   }
 
-  // lane (l16, lq) holds columns 4 lq .. + 3 of tile row 16 i + l16
+  // lane (l16, lq) holds columns 4 lq .. + 3 of tile row 16 m + l16
   __syncthreads();
-  f32x4* sums = reinterpret_cast<f32x4*>(lds);               // [wavefront][tile row][4]
+  f32x4* parts = reinterpret_cast<f32x4*>(lds);              // [wavefront][tile row][4 NT]
 #pragma unroll
-  for (int i = 0; i < MT; ++i) sums[(wave * 16 * MT + 16 * i + l16) * 4 + lq] = acc[i];
+  for (int m = 0; m < MT; ++m)
+#pragma unroll
+    for (int n = 0; n < NT; ++n) parts[((wave * MT + m) * 16 + l16) * 4 * NT + 4 * n + lq] = acc[m][n];
   __syncthreads();
-  for (int e = t; e < rows * 4; e += 512) {
-    const int r = e >> 2, q = e & 3;
+  for (int e = t; e < rows * 4 * NT; e += 64 * NW) {
+    const int r = e / (4 * NT), q = e % (4 * NT);
     f32x4 c{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
     for (int k = 0; k < PIECES; ++k) {
       f32x4 piece{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-      for (int i = 0; i < NW; ++i) piece += sums[(i * 16 * MT + PIECES * r + k) * 4 + q];
+      for (int i = 0; i < NW; ++i) piece += parts[(i * 16 * MT + PIECES * r + k) * 4 * NT + q];
       c += piece;
     }
-    const int n = 16 * tile + 4 * q;
+    const int n = 16 * tile0 + 4 * q;
     if (n < p.N) finish4(p, row0 + r, n, c);
   }
 }
 
 // ------------------------------------------------------------------------------------------------ many rows
-// 128 tile rows x 128 columns, four wavefronts of 64 x 64; the rows of a block of 128 k are staged through registers (where fp32
-// ones are split) into one of two LDS panels while the other is multiplied, weights go from memory into registers and are unpacked
-// by the wavefront that multiplies them, a block ahead.
-template <int GPB, int ROWS>
-__global__ __launch_bounds__(256) void many_kernel(Args p) {
-  constexpr int kPanel = 128 * 256, PIECES = pieces(ROWS), kRealRows = 128 / PIECES;
+// 64 tile rows x 128 columns, four wavefronts of 64 x 32, two workgroups to a CU whose phases overlap (one for groups of 32
+// or odd rows, whose registers two do not leave); the rows of a block of 128 k
+// are staged through registers (where fp32 ones are split) into one of two LDS panels while the other is multiplied; weights go from memory into registers
+// two blocks ahead, as rows do, and are unpacked by the wavefronts that multiply them.
+template <int GPB, int ROWS, bool VEC>
+__global__ __launch_bounds__(256, GPB < 4 && VEC ? 2 : 1) void many_kernel(Args p) {
+  constexpr int kRows = kManyRows, kPanel = kRows * 256, PIECES = pieces(ROWS), kRealRows = kRows / PIECES;
   constexpr int kChunks = (kRealRows * 16 + 255) / 256;
   __shared__ __align__(1024) unsigned char lds[2 * kPanel];
   const int t = threadIdx.x, lane = t & 63, wave = __builtin_amdgcn_readfirstlane(t >> 6), l16 = lane & 15, lq = lane >> 4;
-  const int wm = wave >> 1, wn = wave & 1;
-  const int M = p.count ? *p.count : p.R;
+  const int wn = wave;
+  const int M = p.count ? (*p.count < p.R ? *p.count : p.R) : p.R;
+  // the row groups of 128 columns run on the same XCD, one after the other: its L2 serves the weights to all but the first
   const int coltiles = (p.ntiles + 7) / 8, groups = gridDim.x / ((coltiles + 7) / 8 * 8), id = blockIdx.x >> 3;
   const int ct = (id / groups) * 8 + (blockIdx.x & 7), group = id % groups;
   const int row0 = group * kRealRows, rows = M - row0 < kRealRows ? M - row0 : kRealRows;
   if (ct >= coltiles || rows <= 0) return;
   typedef typename Chunk<ROWS>::Raw Raw;
-  Raw x[kChunks];
+  Raw x[2][kChunks];
   int src[kChunks];
 #pragma unroll
   for (int i = 0; i < kChunks; ++i) {
     int r = (256 * i + t) >> 4;
-    if (r >= rows) r = rows - 1;                 // rows past the last repeat it: their sums are not stored
+    if (r >= rows) r = rows - 1;                 // rows past the last repeat it: their sums are not used
     src[i] = p.gather ? p.rowidx[row0 + r] : row0 + r;
   }
-  if (PIECES * kRealRows < 128)                  // tile rows that no piece fills
-    for (int i = t; i < (128 - PIECES * kRealRows) * 16; i += 256)
+  int64_t at[2];                                 // first block of this wavefront's 2 x 16 columns
 #pragma unroll
-      for (int h = 0; h < 2; ++h) *reinterpret_cast<u32x4*>(lds + h * kPanel + PIECES * kRealRows * 256 + 16 * i) = u32x4{0, 0, 0, 0};
-  auto fetch_rows = [&](int b) {
-#pragma unroll
-    for (int i = 0; i < kChunks; ++i) load_chunk<ROWS>(p, src[i], 128 * b + 8 * l16, x[i]);
+  for (int n = 0; n < 2; ++n) {
+    const int nt = ct * 8 + wn * 2 + n;
+    at[n] = static_cast<int64_t>(nt < p.ntiles ? nt : p.ntiles - 1) * p.kblocks;
+  }
+  u32x4 w[2][2];
+  u32x2 s[2][2][GPB];
+  // the blocks in the order of the sum, for the multiplication (b) and, ahead of it, for the loads of rows and weights; past the
+  // last block some block is requested again: no branch between the loads, which the compiler could only wait out
+  auto advance = [&](int b) {
+    const int next = b + kShares < p.kblocks ? b + kShares : b % kShares + 1;
+    return next < p.kblocks ? next : b;
   };
-  auto put_rows = [&](int h) {
+  int bx = 0, bw = 0, b = 0;
+  auto fetch_rows = [&](Raw (&x)[kChunks]) {
+#pragma unroll
+    for (int i = 0; i < kChunks; ++i) load_chunk<ROWS, VEC>(p, src[i], 128 * bx + 8 * l16, x[i]);
+    bx = advance(bx);
+  };
+  auto put_rows = [&](int h, int block, Raw (&x)[kChunks]) {
 #pragma unroll
     for (int i = 0; i < kChunks; ++i)
-      if ((256 * i + t) >> 4 < kRealRows) put_chunk<ROWS>(lds + h * kPanel, (256 * i + t) >> 4, l16, x[i]);
+      if (256 * kChunks <= 16 * kRealRows || (256 * i + t) >> 4 < kRealRows)
+        put_chunk<ROWS>(lds + h * kPanel, (256 * i + t) >> 4, l16, VEC && 128 * block + 128 > p.K ? zero_if<ROWS>(128 * block + 8 * l16 >= p.K, x[i]) : x[i]);
   };
-  u32x4 w[4], wnext[4];
-  u32x2 s[4][GPB], snext[4][GPB];
-  auto fetch_weights = [&](int b, u32x4 (&w)[4], u32x2 (&s)[4][GPB]) {
+  auto fetch_weights = [&](u32x4 (&w)[2], u32x2 (&s)[2][GPB]) {
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      int nt = ct * 8 + wn * 4 + i;
-      if (nt >= p.ntiles) nt = p.ntiles - 1;
-      const int64_t at = static_cast<int64_t>(nt) * p.kblocks + b;
-      w[i] = p.W[at * 64 + lane];
+    for (int n = 0; n < 2; ++n) {
+      w[n] = p.W[(at[n] + bw) * 64 + lane];
 #pragma unroll
-      for (int g = 0; g < GPB; ++g) s[i][g] = *reinterpret_cast<const u32x2*>(p.S + (at * GPB + g) * 16 + 4 * lq);
+      for (int g = 0; g < GPB; ++g) s[n][g] = *reinterpret_cast<const u32x2*>(p.S + ((at[n] + bw) * GPB + g) * 16 + 4 * lq);
     }
+    bw = advance(bw);
   };
-  f32x4 acc[4][4], total[4][4];
-#pragma unroll
-  for (int i = 0; i < 16; ++i) acc[i >> 2][i & 3] = total[i >> 2][i & 3] = f32x4{0.f, 0.f, 0.f, 0.f};
-  fetch_rows(0);
-  fetch_weights(0, w, s);
-  put_rows(0);
-  __syncthreads();
+  f32x4 acc[4][2] = {}, total[4][2] = {};
   const bf16x8 m8 = minus8();
-  for (int b = 0, step = 0; step < p.kblocks; ++step) {
-    int next = b + kShares;                      // the last block of a share: its sum is complete
-    const bool share_ends = next >= p.kblocks, more = step + 1 < p.kblocks;
-    if (share_ends) next = b % kShares + 1;
-    if (more) {
-      fetch_rows(next);
-      fetch_weights(next, wnext, snext);
-    }
-    const unsigned char* panel = lds + (step & 1) * kPanel;
+  fetch_rows(x[0]);
+  fetch_weights(w[0], s[0]);
+  fetch_rows(x[1]);
+  fetch_weights(w[1], s[1]);
+  put_rows(0, 0, x[0]);
+  fetch_rows(x[0]);
+  __syncthreads();
+  // step i of the sum from panel i & 1; the next step's rows, requested two steps ago, are written to the other panel meanwhile
+  auto step = [&](int i, int h) {
+    const int next = advance(b);
+    put_rows(h ^ 1, next, x[h ^ 1]);             // (after the last step: not read)
+    fetch_rows(x[h ^ 1]);
+    const unsigned char* panel = lds + h * kPanel;
 #pragma unroll
     for (int g = 0; g < GPB; ++g) {
       constexpr int J = 4 / GPB;
       bf16x8 xf[4][J];
-      f32x4 c0[4];
+      f32x4 c[4][2];
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        c0[i] = f32x4{0.f, 0.f, 0.f, 0.f};
+      for (int j = 0; j < J; ++j)
 #pragma unroll
-        for (int j = 0; j < J; ++j) {
-          xf[i][j] = get_fragment(panel, wm * 64 + 16 * i, g * J + j, l16, lq);
-          c0[i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(m8, xf[i][j], c0[i], 0, 0, 0);
+        for (int m = 0; m < 4; ++m) {
+          xf[m][j] = get_fragment(panel, 16 * m, g * J + j, l16, lq);
+          c[m][0] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(m8, xf[m][j], j ? c[m][0] : f32x4{0.f, 0.f, 0.f, 0.f}, 0, 0, 0);
         }
+#pragma unroll
+      for (int m = 0; m < 4; ++m) c[m][1] = c[m][0];
+      // eight independent chains side by side
+#pragma unroll
+      for (int j = 0; j < J; ++j) {
+        bf16x8 wf[2];
+#pragma unroll
+        for (int n = 0; n < 2; ++n) wf[n] = unpack(w[h][n][g * J + j]);
+#pragma unroll
+        for (int m = 0; m < 4; ++m)
+#pragma unroll
+          for (int n = 0; n < 2; ++n) c[m][n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wf[n], xf[m][j], c[m][n], 0, 0, 0);
       }
 #pragma unroll
-      for (int n = 0; n < 4; ++n) {
-        bf16x8 wf[J];
+      for (int n = 0; n < 2; ++n) {
+        const f32x4 sc = scales4(s[h][n][g]);
 #pragma unroll
-        for (int j = 0; j < J; ++j) wf[j] = unpack(w[n][g * J + j]);
-        const f32x4 sc = scales4(s[n][g]);
-        f32x4 c[4];
-#pragma unroll
-        for (int i = 0; i < 4; ++i) c[i] = c0[i];
-#pragma unroll
-        for (int j = 0; j < J; ++j)
-#pragma unroll
-          for (int i = 0; i < 4; ++i) c[i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wf[j], xf[i][j], c[i], 0, 0, 0);
-#pragma unroll
-        for (int i = 0; i < 4; ++i) acc[i][n] = add_scaled(acc[i][n], sc, c[i]);
+        for (int m = 0; m < 4; ++m) acc[m][n] = add_scaled(acc[m][n], sc, c[m][n]);
       }
+      if (GPB > 1) __builtin_amdgcn_sched_barrier(0);       // the groups one after the other: registers
     }
-    if (share_ends) {
+    fetch_weights(w[h], s[h]);
+    if (b + kShares >= p.kblocks) {              // the last block of a share: its sum is complete
 #pragma unroll
-      for (int i = 0; i < 4; ++i)
+      for (int m = 0; m < 4; ++m)
 #pragma unroll
-        for (int n = 0; n < 4; ++n) {
-          total[i][n] += acc[i][n];
-          acc[i][n] = f32x4{0.f, 0.f, 0.f, 0.f};
+        for (int n = 0; n < 2; ++n) {
+          total[m][n] += acc[m][n];
+          acc[m][n] = f32x4{0.f, 0.f, 0.f, 0.f};
         }
     }
     b = next;
-    if (more) {
-      put_rows((step + 1) & 1);
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        w[i] = wnext[i];
-#pragma unroll
-        for (int g = 0; g < GPB; ++g) s[i][g] = snext[i][g];
-      }
-    }
-    __syncthreads();
+    ldsring::barrier_keep_loads();               // __syncthreads would wait for the loads in flight
+  };
+  for (int i = 0; i < p.kblocks; i += 2) {
+    step(i, 0);
+    if (i + 1 < p.kblocks) step(i + 1, 1);
   }
   if constexpr (PIECES == 1) {
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-      const int r = wm * 64 + 16 * i + l16;
+      const int r = 16 * i + l16;
       if (r >= rows) continue;
 #pragma unroll
-      for (int n = 0; n < 4; ++n) {
-        const int col = (ct * 8 + wn * 4 + n) * 16 + 4 * lq;
+      for (int n = 0; n < 2; ++n) {
+        const int col = (ct * 8 + wn * 2 + n) * 16 + 4 * lq;
         if (col < p.N) finish4(p, row0 + r, col, total[i][n]);
       }
     }
   } else {
-    // the pieces of a row are neighbouring tile rows: 64 KiB of LDS hold the tile for the sum
-    f32x4* sums = reinterpret_cast<f32x4*>(lds);             // [tile row][32 groups of 4 columns]
+    // the pieces of a row are neighbouring tile rows: the panels' 32 KiB hold the tile for their sum
+    f32x4* parts = reinterpret_cast<f32x4*>(lds);            // [tile row][32 groups of 4 columns]
 #pragma unroll
     for (int i = 0; i < 4; ++i)
 #pragma unroll
-      for (int n = 0; n < 4; ++n) sums[(wm * 64 + 16 * i + l16) * 32 + (wn * 4 + n) * 4 + lq] = total[i][n];
+      for (int n = 0; n < 2; ++n) parts[(16 * i + l16) * 32 + (wn * 2 + n) * 4 + lq] = total[i][n];
     __syncthreads();
     for (int e = t; e < rows * 32; e += 256) {
       const int r = e >> 5, q = e & 31, col = ct * 128 + 4 * q;
-      const f32x4 c = (sums[(3 * r) * 32 + q] + sums[(3 * r + 1) * 32 + q]) + sums[(3 * r + 2) * 32 + q];
+      f32x4 c{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int k = 0; k < PIECES; ++k) c += parts[(PIECES * r + k) * 32 + q];
       if (col < p.N) finish4(p, row0 + r, col, c);
     }
   }

@@ -48,6 +48,20 @@ __device__ __forceinline__ double lane_xor(double v) {
   return __longlong_as_double((static_cast<long long>(hi) << 32) | static_cast<unsigned int>(lo));
 }
 
+// v + (v of lane ^ MASK), and the sum over the wavefront that these make: the same bits on all lanes.
+template <int MASK>
+__device__ __forceinline__ float xor_add(float v) {
+  return v + __int_as_float(lane_xor<MASK>(__float_as_int(v)));
+}
+__device__ __forceinline__ float wave_sum(float v) {
+  v = xor_add<1>(v);
+  v = xor_add<2>(v);
+  v = xor_add<4>(v);
+  v = xor_add<8>(v);
+  v = xor_add<16>(v);
+  return xor_add<32>(v);
+}
+
 // v + (v of lane ^ MASK) for the two row-swap masks: after the swap the two results hold the two addends in
 // the same order on both partners, so no select is needed and the sum has the same bits on both.
 template <int MASK>

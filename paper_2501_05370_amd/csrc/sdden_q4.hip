@@ -72,7 +72,8 @@ int sdden_q4_destroy(sdden_q4* m) {
 // ------------------------------------------------------------------------------------------------ the MLP denoiser in 4 bits
 // The network of sdden_mlp.hip with its three matrices in 4 bits, as a draft model that reads a quarter of the target's bytes:
 //   compact_rows     unmasked rows -> dense list
-//   product 1        H1 = silu(X Q1 + tb[krow])    rows gathered, rounded to bf16 as they enter (or the caller's bf16 image)
+//   product 1        H1 = silu(X Q1 + tb[krow])    rows gathered from the caller's bf16 image, or rounded to bf16 as they enter
+//                    (more than 32 rows: by gather_round)
 //   product 2        H2 = silu(H1 Q2 + b2)
 //   product 3        out[rowidx] = H2 Q3 + b3       fp32
 namespace {
@@ -117,27 +118,49 @@ void quantize(const uint16_t* W, int K, int N, int group, std::vector<uint8_t>& 
   }
 }
 
+// Xb[m] = X[rowidx[m]] rounded to bf16, rows of ld (16 bytes) apart
+__global__ __launch_bounds__(256) void gather_round_kernel(const float* __restrict__ X, const int32_t* __restrict__ rowidx,
+                                                           const int32_t* __restrict__ count, uint16_t* __restrict__ Xb, int d, int64_t ld) {
+  const int per_row = (d + 3) / 4;
+  const int64_t total = static_cast<int64_t>(*count) * per_row;
+  for (int64_t g = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x; g < total; g += static_cast<int64_t>(gridDim.x) * 256) {
+    const int m = static_cast<int>(g / per_row), c = static_cast<int>(g % per_row) * 4;
+    const float* x = X + static_cast<int64_t>(rowidx[m]) * d + c;
+    q4::f32x4 v{0.f, 0.f, 0.f, 0.f};
+    if (d % 4 == 0) {
+      v = *reinterpret_cast<const q4::f32x4*>(x);
+    } else {
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+        if (c + e < d) v[e] = x[e];
+    }
+    *reinterpret_cast<q4::u32x2*>(Xb + m * ld + c) = lgemm::pack_bf16(v);
+  }
+}
+
 struct Mlp4Denoiser final : sdden {
   int H = 0, cap_rows = 0;
   sdden_q4 Q1, Q2, Q3;
   float *tb = nullptr, *b2 = nullptr, *b3 = nullptr;      // [T,H], [H], [d]
   int32_t *rowidx = nullptr, *count = nullptr;
-  uint16_t *H1 = nullptr, *H2 = nullptr;
-  int64_t ldh = 0;                                        // rows of H1 and H2 start on 16 bytes
+  uint16_t *Xb = nullptr, *H1 = nullptr, *H2 = nullptr;
+  int64_t ldx = 0, ldh = 0;                               // rows of Xb, of H1 and H2 start on 16 bytes
 
   ~Mlp4Denoiser() override {
     for (void* p : {static_cast<void*>(tb), static_cast<void*>(b2), static_cast<void*>(b3), static_cast<void*>(rowidx),
-                    static_cast<void*>(count), static_cast<void*>(H1), static_cast<void*>(H2)})
+                    static_cast<void*>(count), static_cast<void*>(Xb), static_cast<void*>(H1), static_cast<void*>(H2)})
       if (p) (void)hipFree(p);
   }
 
   int reserve(int R) override {
     if (R <= cap_rows) return SD_OK;
-    for (void* p : {static_cast<void*>(rowidx), static_cast<void*>(H1), static_cast<void*>(H2)})
+    for (void* p : {static_cast<void*>(rowidx), static_cast<void*>(Xb), static_cast<void*>(H1), static_cast<void*>(H2)})
       if (p) (void)hipFree(p);
-    rowidx = nullptr; H1 = H2 = nullptr; cap_rows = 0;
+    rowidx = nullptr; Xb = H1 = H2 = nullptr; cap_rows = 0;
+    ldx = (d + 7) / 8 * 8;
     ldh = (H + 7) / 8 * 8;
     SD_HIP_TRY(err, hipMalloc(&rowidx, 4 * static_cast<size_t>(R)));
+    if (R > q4::kRoundedRows) SD_HIP_TRY(err, hipMalloc(&Xb, 2 * static_cast<size_t>(R) * ldx));
     SD_HIP_TRY(err, hipMalloc(&H1, 2 * static_cast<size_t>(R) * ldh));
     SD_HIP_TRY(err, hipMalloc(&H2, 2 * static_cast<size_t>(R) * ldh));
     if (!count) SD_HIP_TRY(err, hipMalloc(&count, 4));
@@ -150,20 +173,32 @@ struct Mlp4Denoiser final : sdden {
     return go(R, X, Xb, krow, out, st);
   }
 
-  int go(int R, const float* X, const uint16_t* Xb, const int32_t* krow, float* out, hipStream_t st) {
+  int go(int R, const float* X, const uint16_t* image, const int32_t* krow, float* out, hipStream_t st) {
     if (R > cap_rows)
       return sdi::fail(err, SD_ERR_WORKSPACE, "sdden_eval(mlp4): %d rows exceed the %d reserved (sdden_reserve)", R, cap_rows);
-    if (!sdi::aligned16(X) || !sdi::aligned16(out) || !sdi::aligned16(Xb))
+    if (!sdi::aligned16(X) || !sdi::aligned16(out) || !sdi::aligned16(image))
       return sdi::fail(err, SD_ERR_ARG, "sdden_eval(mlp4): X, its image and out must be 16-byte aligned");
     hipLaunchKernelGGL(sdrows::compact_rows_kernel, dim3(sdrows::compact_rows_grid(R)), dim3(sdrows::kScan), 0, st, krow, rowidx, count,
                        active, rows_per_chain, R, T);
     q4::Args a{};
     Q1.fill(a);
-    a.X = Xb ? static_cast<const void*>(Xb) : X; a.ldx = d; a.R = R; a.vec = d % (Xb ? 8 : 4) == 0;
-    a.bias = tb; a.krow = krow; a.rowidx = rowidx; a.count = count; a.gather = true; a.silu = true;
+    a.R = R;
+    int form = q4::kBf16;
+    if (image) {
+      a.X = image; a.ldx = d; a.vec = d % 8 == 0; a.gather = true;
+    } else if (R <= q4::kRoundedRows) {
+      a.X = X; a.ldx = d; a.vec = d % 4 == 0; a.gather = true;
+      form = q4::kF32Rounded;
+    } else {
+      const int64_t chunks = static_cast<int64_t>(R) * ((d + 3) / 4);
+      hipLaunchKernelGGL(gather_round_kernel, dim3(static_cast<unsigned>(std::min<int64_t>((chunks + 255) / 256, 256 * 32))), dim3(256), 0, st, X,
+                         rowidx, count, Xb, d, ldx);
+      a.X = Xb; a.ldx = ldx; a.vec = true;
+    }
+    a.bias = tb; a.krow = krow; a.rowidx = rowidx; a.count = count; a.silu = true;
     a.Y = H1; a.ldy = ldh; a.vec_out = true;
     prof.mark(1, st);
-    SD_HIP_TRY(err, Q1.launch(a, R, Xb ? q4::kBf16 : q4::kF32Rounded, st));
+    SD_HIP_TRY(err, Q1.launch(a, R, form, st));
     prof.mark(1, st);
     a = q4::Args{};
     Q2.fill(a);
