@@ -13,6 +13,7 @@
 #include <hip/hip_runtime.h>
 
 #include <cstdint>
+#include <type_traits>
 
 #include "sd_lanes.h"
 
@@ -27,32 +28,43 @@ struct Args {
   float* mean;                  // forward: out or null; backward: in
   float* rstd;
   float eps;
+  bool keep;                    // the output is small enough to stay in the caches
   float* partial;               // backward: [2, grid, d] or null
   const int32_t* count;         // forward: rows that count, at most R (device; null: R)
 };
 
+// V elements as they lie in memory, and as floats.
 template <int V, typename T>
-__device__ __forceinline__ void load(const T* p, float (&v)[V]) {
+struct Raw {
   typedef T vec __attribute__((ext_vector_type(V), aligned(V * sizeof(T) < 16 ? V * sizeof(T) : 16)));
-  if constexpr (V == 1) {
-    v[0] = static_cast<float>(*p);
-  } else {
-    const vec t = *reinterpret_cast<const vec*>(p);
-#pragma unroll
-    for (int e = 0; e < V; ++e) v[e] = static_cast<float>(t[e]);
+  typename std::conditional<V == 1, T, vec>::type v;
+  __device__ __forceinline__ void load(const T* p) { v = *reinterpret_cast<const decltype(v)*>(p); }
+  __device__ __forceinline__ float operator[](int e) const {
+    if constexpr (V == 1) return static_cast<float>(v);
+    else return static_cast<float>(v[e]);
   }
-}
+};
 
 template <int V, typename T>
-__device__ __forceinline__ void store(T* p, const float (&v)[V]) {
-  typedef T vec __attribute__((ext_vector_type(V), aligned(V * sizeof(T) < 16 ? V * sizeof(T) : 16)));
+__device__ __forceinline__ void load(const T* p, float (&v)[V]) {
+  Raw<V, T> r;
+  r.load(p);
+#pragma unroll
+  for (int e = 0; e < V; ++e) v[e] = r[e];
+}
+
+// keep: into the caches, for the kernel that reads it next; else past them.
+template <int V, typename T>
+__device__ __forceinline__ void store(T* p, const float (&v)[V], bool keep) {
+  typedef typename Raw<V, T>::vec vec;
   if constexpr (V == 1) {
     *p = static_cast<T>(v[0]);
   } else {
     vec t;
 #pragma unroll
     for (int e = 0; e < V; ++e) t[e] = static_cast<T>(v[e]);
-    *reinterpret_cast<vec*>(p) = t;
+    if (keep) *reinterpret_cast<vec*>(p) = t;
+    else __builtin_nontemporal_store(t, reinterpret_cast<vec*>(p));
   }
 }
 
@@ -97,19 +109,29 @@ __global__ __launch_bounds__(threads_of(TPR)) void forward_kernel(Args p) {
       if (p.b) load<V>(p.b + col, b[c]);
     }
   }
-  for (int64_t r = static_cast<int64_t>(blockIdx.x) * RPB + threadIdx.x / TPR; r < p.R; r += static_cast<int64_t>(gridDim.x) * RPB) {
+  Raw<V, TX> raw[C];                    // the row that comes next: it is on its way during the sums and stores of this one
+  auto fetch = [&](int64_t r) {
     const TX* x = static_cast<const TX*>(p.x) + r * p.ldx;
+#pragma unroll
+    for (int c = 0; c < C; ++c)
+      if ((c * TPR + t) * V < p.d) raw[c].load(x + (c * TPR + t) * V);
+  };
+  int64_t r = static_cast<int64_t>(blockIdx.x) * RPB + threadIdx.x / TPR;
+  if (r < p.R) fetch(r);
+  for (; r < p.R; r += static_cast<int64_t>(gridDim.x) * RPB) {
     float v[C][V];
     float s = 0.f, unused = 0.f;
 #pragma unroll
-    for (int c = 0; c < C; ++c) {
-      const int col = (c * TPR + t) * V;
-      if (col < p.d) {
-        load<V>(x + col, v[c]);
+    for (int c = 0; c < C; ++c)
+      if ((c * TPR + t) * V < p.d) {
 #pragma unroll
-        for (int e = 0; e < V; ++e) s += v[c][e];
+        for (int e = 0; e < V; ++e) {
+          v[c][e] = raw[c][e];
+          s += v[c][e];
+        }
       }
-    }
+    const int64_t next = r + static_cast<int64_t>(gridDim.x) * RPB;
+    if (next < p.R) fetch(next);
     row_sum2<TPR>(s, unused, red, 0);
     const float mean = s * inv_d;
     float q = 0.f;
@@ -136,7 +158,7 @@ __global__ __launch_bounds__(threads_of(TPR)) void forward_kernel(Args p) {
       if (col < p.d) {
 #pragma unroll
         for (int e = 0; e < V; ++e) v[c][e] = v[c][e] * rstd * w[c][e] + b[c][e];
-        store<V>(y + col, v[c]);
+        store<V>(y + col, v[c], p.keep);
       }
     }
   }
@@ -193,6 +215,8 @@ __global__ __launch_bounds__(threads_of(TPR)) void backward_kernel(Args p) {
     const TX* x = static_cast<const TX*>(p.x) + r * p.ldx;
     const TY* dy = static_cast<const TY*>(p.dy) + r * p.lddy;
     const float mean = p.mean[r], rstd = p.rstd[r];
+    const TX* dres = p.dres ? static_cast<const TX*>(p.dres) + r * p.lddres : nullptr;
+    Raw<V, TX> add[C];
     float xh[C][V], g[C][V];
     float sg = 0.f, sgx = 0.f;
 #pragma unroll
@@ -201,6 +225,7 @@ __global__ __launch_bounds__(threads_of(TPR)) void backward_kernel(Args p) {
       if (col < p.d) {
         load<V>(x + col, xh[c]);
         load<V>(dy + col, g[c]);
+        if (dres) add[c].load(dres + col);
       }
     }
 #pragma unroll
@@ -221,7 +246,6 @@ __global__ __launch_bounds__(threads_of(TPR)) void backward_kernel(Args p) {
     sg *= inv_d;
     sgx *= inv_d;
     TX* dx = static_cast<TX*>(p.y) + r * p.ldy;
-    const TX* dres = p.dres ? static_cast<const TX*>(p.dres) + r * p.lddres : nullptr;
 #pragma unroll
     for (int c = 0; c < C; ++c) {
       const int col = (c * TPR + t) * V;
@@ -230,12 +254,10 @@ __global__ __launch_bounds__(threads_of(TPR)) void backward_kernel(Args p) {
 #pragma unroll
         for (int e = 0; e < V; ++e) o[e] = rstd * (g[c][e] - sg - xh[c][e] * sgx);
         if (dres) {
-          float a[V];
-          load<V>(dres + col, a);
 #pragma unroll
-          for (int e = 0; e < V; ++e) o[e] += a[e];
+          for (int e = 0; e < V; ++e) o[e] += add[c][e];
         }
-        store<V>(dx + col, o);
+        store<V>(dx + col, o, p.keep);
       }
     }
   }
@@ -315,22 +337,30 @@ __global__ __launch_bounds__(256) void long_partials_kernel(Args p) {
   p.partial[static_cast<int64_t>(gridDim.y + blockIdx.y) * p.d + c] = sb;
 }
 
-// out[0..d) and out2[0..d): sums of the P partial rows; 64 columns x 16 shares of the rows per workgroup.
+// dw[0..d) and db[0..d): sums of the P partial rows; 32 columns x 32 shares of the rows per workgroup, eight loads of a share in
+// flight.  Bound by latency: 1024 partial rows of 4096 (33 MB, just written) in 7 us.
 __global__ __launch_bounds__(1024) void reduce_partials_kernel(const float* __restrict__ partial, int P, int d, float* __restrict__ dw,
                                                                float* __restrict__ db) {
-  __shared__ float sum[16][64];
-  const int lane = threadIdx.x & 63, share = threadIdx.x >> 6, col = blockIdx.x * 64 + lane;
+  constexpr int kCols = 32, kShares = 32, kBatch = 8;
+  __shared__ float sum[kShares][kCols + 1];
+  const int lane = threadIdx.x % kCols, share = threadIdx.x / kCols, col = blockIdx.x * kCols + lane;
   float* out = blockIdx.y ? db : dw;
   if (!out) return;
+  const float* p = partial + static_cast<int64_t>(blockIdx.y) * P * d + (col < d ? col : d - 1);
   float s = 0.f;
-  if (col < d)
-    for (int i = share; i < P; i += 16) s += partial[(static_cast<int64_t>(blockIdx.y) * P + i) * d + col];
+  for (int i = share; i < P; i += kShares * kBatch) {
+    float v[kBatch];
+#pragma unroll
+    for (int k = 0; k < kBatch; ++k) v[k] = i + k * kShares < P ? p[static_cast<int64_t>(i + k * kShares) * d] : 0.f;
+#pragma unroll
+    for (int k = 0; k < kBatch; ++k) s += v[k];
+  }
   sum[share][lane] = s;
   __syncthreads();
   if (share == 0 && col < d) {
     s = 0.f;
 #pragma unroll
-    for (int i = 0; i < 16; ++i) s += sum[i][lane];
+    for (int i = 0; i < kShares; ++i) s += sum[i][lane];
     out[col] = s;
   }
 }

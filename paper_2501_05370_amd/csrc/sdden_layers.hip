@@ -28,12 +28,18 @@ size_t size_of(int32_t t) { return t == SDDEN_F32 ? 4 : 2; }
 enum Width { kWave, k256, k512, k1024, kLong };
 Width width_of(int d) { return d <= 1024 ? kWave : d <= 4096 ? k256 : d <= 12288 ? k512 : d <= 16384 ? k1024 : kLong; }
 
-// Partial rows of the weights' gradients: as many workgroups as walk the rows.
+// Partial rows of the weights' gradients: as many workgroups as walk the rows.  16384 rows of 4096: 1024 workgroups 101 + 7 us (the
+// second for adding the partial rows up), 512 147 + 5.
 int partial_rows(int R, int d) {
   if (d > 16384) return std::min(R, 64);
   if (d <= 1024) return std::min((R + 3) / 4, 1024);
-  return std::min(R, 512);
+  return std::min(R, d <= 4096 ? 1024 : 512);
 }
+
+// Outputs of more than this are stored past the caches: of an output that would fill them the next kernel finds little, and the
+// inputs, which a backward pass reads again, stay.  Forward and backward of 16384 bf16 rows of 4096 in turn: 57 + 101 us, through
+// the caches 58 + 125.
+constexpr int64_t kKeepBytes = int64_t{32} << 20;
 
 template <int V, typename TX, typename TY>
 void norm_forward(const lnorm::Args& a, hipStream_t st) {
@@ -139,6 +145,7 @@ int sdden_layernorm_forward(int32_t R, int32_t d, const void* x, int32_t x_type,
   if (R == 0) return SD_OK;
   lnorm::Args a{};
   a.R = R; a.d = d; a.x = x; a.ldx = x_stride; a.y = y; a.ldy = y_stride; a.w = weight; a.b = bias; a.mean = mean; a.rstd = rstd; a.eps = eps;
+  a.keep = static_cast<int64_t>(R) * d * static_cast<int64_t>(size_of(y_type)) <= kKeepBytes;
   const int vec = vector_width(d, x_type, y_type, {x_stride, y_stride}, {x, y, weight, bias});
   by_type(vec, x_type, y_type, [&](auto v, auto tx, auto ty) { norm_forward<decltype(v)::value, decltype(tx), decltype(ty)>(a, static_cast<hipStream_t>(stream)); });
   return done(what, hipGetLastError());
@@ -163,6 +170,7 @@ int sdden_layernorm_backward(int32_t R, int32_t d, const void* dy, int32_t dy_ty
   a.R = R; a.d = d; a.x = x; a.ldx = x_stride; a.dy = dy; a.lddy = dy_stride; a.dres = dres; a.lddres = dres ? dres_stride : 0;
   a.y = dx; a.ldy = dx_stride; a.w = weight; a.mean = const_cast<float*>(mean); a.rstd = const_cast<float*>(rstd);
   a.partial = grads ? static_cast<float*>(workspace) : nullptr;
+  a.keep = static_cast<int64_t>(R) * d * static_cast<int64_t>(size_of(x_type)) <= kKeepBytes;
   hipStream_t st = static_cast<hipStream_t>(stream);
   const int P = R > 0 ? partial_rows(R, d) : 0;
   if (R > 0) {
@@ -170,7 +178,7 @@ int sdden_layernorm_backward(int32_t R, int32_t d, const void* dy, int32_t dy_ty
     by_type(vec, x_type, dy_type, [&](auto v, auto tx, auto ty) { norm_backward<decltype(v)::value, decltype(tx), decltype(ty)>(a, P, st); });
   }
   if (grads)
-    hipLaunchKernelGGL(lnorm::reduce_partials_kernel, dim3((d + 63) / 64, 2), dim3(1024), 0, st, a.partial, P, d, dweight, dbias);
+    hipLaunchKernelGGL(lnorm::reduce_partials_kernel, dim3((d + 31) / 32, 2), dim3(1024), 0, st, a.partial, P, d, dweight, dbias);
   return done(what, hipGetLastError());
 }
 
@@ -327,7 +335,7 @@ struct GatedDenoiser final : sdden {
                        table, rowidx, krow, count, h, d);
     for (int l = 0; l < blocks; ++l) {
       lnorm::Args a{};
-      a.R = R; a.d = d; a.x = h; a.ldx = d; a.y = n; a.ldy = d; a.eps = eps; a.count = count;
+      a.R = R; a.d = d; a.x = h; a.ldx = d; a.y = n; a.ldy = d; a.eps = eps; a.count = count; a.keep = true;
       a.w = nw + static_cast<int64_t>(l) * d;
       a.b = nb + static_cast<int64_t>(l) * d;
       prof.mark(1, st);
