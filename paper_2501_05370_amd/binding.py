@@ -480,44 +480,52 @@ class Denoiser:
             pass
 
 
-# -- layers of row networks: functions of tensors on the current device, on its current stream
-_LAYER_TYPES = {torch.float32: SDDEN_F32, torch.bfloat16: SDDEN_BF16}
+# -- layers of row networks: functions of tensors on the current device, on its current stream.  Calls on few rows are bound by
+# the host, so the checks ask each tensor once and build their messages only when one fails.
+_F32, _BF16 = torch.float32, torch.bfloat16
+_LAYER_TYPES = {_F32: SDDEN_F32, _BF16: SDDEN_BF16}
 
 
-def _rows(t: Optional[torch.Tensor], name: str, shape=None, types=(torch.float32, torch.bfloat16), allow_none: bool = False):
-    """(pointer, stride between rows) of a matrix whose rows are contiguous and need not follow each other."""
-    if t is None and allow_none:
-        return None, 0
-    if t is None or not t.is_cuda or t.device.index != torch._C._cuda_getDevice() or t.dtype not in types or t.dim() != 2:
-        raise SDError(f"{name}: need a matrix of {types} on the current device, got "
-                      + ("None" if t is None else f"{t.dtype} {tuple(t.shape)} on {t.device}"))
-    if shape is not None and tuple(t.shape) != tuple(shape):
-        raise SDError(f"{name}: need shape {tuple(shape)}, got {tuple(t.shape)}")
-    R, d = t.shape
-    if d > 1 and t.stride(1) != 1:
+def _rows(t: Optional[torch.Tensor], name: str, shape=None, only=None, allow_none: bool = False):
+    """(pointer, stride between rows) of an fp32 or bf16 matrix (or of type ``only``) whose rows are contiguous and need not follow
+    each other."""
+    if t is None:
+        if allow_none:
+            return None, 0
+        raise SDError(f"{name}: tensor required")
+    dims, dtype = t.shape, t.dtype
+    if not t.is_cuda or t.get_device() != torch._C._cuda_getDevice() or len(dims) != 2 or (dtype is not only if only is not None else dtype not in _LAYER_TYPES):
+        raise SDError(f"{name}: need a matrix of {only or 'fp32 or bf16'} on the current device, got {dtype} {tuple(dims)} on {t.device}")
+    if shape is not None and dims != shape:
+        raise SDError(f"{name}: need shape {tuple(shape)}, got {tuple(dims)}")
+    R, d = dims
+    stride, inner = t.stride()
+    if inner != 1 and d > 1:
         raise SDError(f"{name}: the elements of a row must be contiguous, got strides {t.stride()}")
-    stride = t.stride(0) if R > 1 else max(d, 1)
-    if stride < d:
+    if R <= 1:
+        stride = d if d > 0 else 1
+    elif stride < d:
         raise SDError(f"{name}: rows overlap (stride {stride} of {d} columns)")
     return t.data_ptr(), stride
 
 
 def _flat(t: Optional[torch.Tensor], name: str, shape, dtype, allow_none: bool = False) -> Optional[int]:
     """Pointer of a contiguous tensor of this shape and type on the current device."""
-    if t is None and allow_none:
-        return None
-    if t is None or not t.is_cuda or t.device.index != torch._C._cuda_getDevice() or t.dtype is not dtype or not t.is_contiguous() \
-            or tuple(t.shape) != tuple(shape):
-        raise SDError(f"{name}: need a contiguous {dtype} tensor of shape {tuple(shape)} on the current device, got "
-                      + ("None" if t is None else f"{t.dtype} {tuple(t.shape)} on {t.device}"))
-    return t.data_ptr()
+    if t is None:
+        if allow_none:
+            return None
+        raise SDError(f"{name}: tensor required")
+    if t.dtype is dtype and t.shape == shape and t.is_contiguous() and t.is_cuda and t.get_device() == torch._C._cuda_getDevice():
+        return t.data_ptr()
+    raise SDError(f"{name}: need a contiguous {dtype} tensor of shape {tuple(shape)} on the current device, got {t.dtype} "
+                  f"{tuple(t.shape)} on {t.device}, contiguous={t.is_contiguous()}")
 
 
 def _scratch(t: Optional[torch.Tensor], name: str):
     """(pointer, bytes) of a caller's workspace, any contiguous tensor."""
     if t is None:
         return None, 0
-    if not t.is_cuda or t.device.index != torch._C._cuda_getDevice() or not t.is_contiguous():
+    if not t.is_cuda or t.get_device() != torch._C._cuda_getDevice() or not t.is_contiguous():
         raise SDError(f"{name}: need a contiguous tensor on the current device")
     return t.data_ptr(), t.numel() * t.element_size()
 
@@ -550,8 +558,8 @@ def sdden_layernorm_backward(dy, x, weight, mean, rstd, dx, dweight=None, dbias=
     xp, xs = _rows(x, "x")
     R, d = x.shape
     dyp, dys = _rows(dy, "dy", (R, d))
-    dxp, dxs = _rows(dx, "dx", (R, d), (x.dtype,))
-    drp, drs = _rows(dres, "dres", (R, d), (x.dtype,), allow_none=True)
+    dxp, dxs = _rows(dx, "dx", (R, d), x.dtype)
+    drp, drs = _rows(dres, "dres", (R, d), x.dtype, True)
     ws, nbytes = _scratch(workspace, "workspace")
     _layer_check(lib, lib.sdden_layernorm_backward(
         R, d, dyp, _LAYER_TYPES[dy.dtype], dys, xp, _LAYER_TYPES[x.dtype], xs, _flat(weight, "weight", (d,), torch.float32, True),
@@ -567,12 +575,12 @@ def sdden_gated_workspace_bytes(R: int, d: int, H: int) -> int:
 def sdden_gated_forward(X, Wg, Wu, Wd, Y, hidden, gates=None, act: int = SDDEN_SILU, res=None):
     """X [R,d], Wg, Wu [H,d], Wd [d,H], hidden [R,H] bf16; Y and res [R,d] fp32 or bf16; gates [2,R,H] fp32 or None."""
     lib = load_library()
-    bf = torch.bfloat16
-    xp, xs = _rows(X, "X", types=(bf,))
+    bf = _BF16
+    xp, xs = _rows(X, "X", only=bf)
     R, d = X.shape
     H = Wg.shape[0]
     yp, ys = _rows(Y, "Y", (R, d))
-    rp, rs = _rows(res, "res", (R, d), (Y.dtype,), allow_none=True)
+    rp, rs = _rows(res, "res", (R, d), Y.dtype, True)
     if res is not None and R > 1 and rs != ys:
         raise SDError(f"res: its rows must lie as far apart as Y's ({ys}), got {rs}")
     _layer_check(lib, lib.sdden_gated_forward(
@@ -585,12 +593,12 @@ def sdden_gated_backward(dY, X, Wg, Wu, Wd, gates, hidden, dX, dWg, dWu, dWd, wo
     """dX [R,d] bf16 or None; dWg, dWu [H,d], dWd [d,H] fp32 or bf16, or all None; workspace: any tensor of
     sdden_gated_workspace_bytes."""
     lib = load_library()
-    bf = torch.bfloat16
-    xp, xs = _rows(X, "X", types=(bf,))
+    bf = _BF16
+    xp, xs = _rows(X, "X", only=bf)
     R, d = X.shape
     H = Wg.shape[0]
-    dyp, dys = _rows(dY, "dY", (R, d), (bf,))
-    dxp, dxs = _rows(dX, "dX", (R, d), (bf,), allow_none=True)
+    dyp, dys = _rows(dY, "dY", (R, d), bf)
+    dxp, dxs = _rows(dX, "dX", (R, d), bf, True)
     tw = torch.float32 if dWg is None else dWg.dtype
     if tw not in _LAYER_TYPES:
         raise SDError(f"dWg: need fp32 or bf16, got {tw}")
