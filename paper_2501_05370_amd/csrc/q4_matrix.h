@@ -10,50 +10,48 @@ constexpr int kMaxDim = 1 << 20;
 
 constexpr int kRoundedRows = 32;      // most rows of a call with kF32Rounded
 
-template <int MT, int GPB, int ROWS, int XC, int PF, bool VEC>
+template <int MT, int GPB, int ROWS, int XC, int PF>
 hipError_t launch_few(const Args& a, int R, hipStream_t st) {
   // 32 columns a workgroup where that still gives every CU one: the rows' panel is written once for both.  us, 32 / 16 columns, 4096 x 12288:
   // 19 rows, groups of 64 19.0 / 22.5; one row, groups of 32 15.8 / 12.6 (registers for one workgroup per CU)
-  if constexpr (MT <= 2 && GPB <= 2 && VEC) {
+  if constexpr (MT <= 2 && GPB <= 2) {
     if (a.ntiles >= 512) {                   // (one group of rows: see launch_rows)
-      hipLaunchKernelGGL((few_kernel<MT, 2, GPB, ROWS, XC, PF, VEC>), dim3((a.ntiles + 1) / 2), dim3(64 * kShares), 0, st, a);
+      hipLaunchKernelGGL((few_kernel<MT, 2, GPB, ROWS, XC, PF>), dim3((a.ntiles + 1) / 2), dim3(64 * kShares), 0, st, a);
       return hipGetLastError();
     }
   }
   constexpr int kRows = 16 * MT / pieces(ROWS);
-  hipLaunchKernelGGL((few_kernel<MT, 1, GPB, ROWS, XC, PF, VEC>), dim3(a.ntiles, (R + kRows - 1) / kRows), dim3(64 * kShares), 0, st, a);
+  hipLaunchKernelGGL((few_kernel<MT, 1, GPB, ROWS, XC, PF>), dim3(a.ntiles, (R + kRows - 1) / kRows), dim3(64 * kShares), 0, st, a);
   return hipGetLastError();
 }
 
-template <int GPB, int ROWS, bool VEC>
+template <int GPB, int ROWS>
 hipError_t launch_rows(const Args& a, int R, hipStream_t st) {
   constexpr int P = pieces(ROWS);
-  if (R <= 4) return launch_few<1, GPB, ROWS, 1, VEC ? 4 : 2, VEC>(a, R, st);
-  if (R <= 16 / P) return launch_few<1, GPB, ROWS, (16 / P + 3) / 4, VEC ? ROWS == kF32Rounded ? 3 : 4 : 1, VEC>(a, R, st);
-  if (R <= 32 / P) return launch_few<2, GPB, ROWS, (32 / P + 3) / 4, VEC ? 2 : 1, VEC>(a, R, st);
+  if (R <= 4) return launch_few<1, GPB, ROWS, 1, 4>(a, R, st);
+  if (R <= 16 / P) return launch_few<1, GPB, ROWS, (16 / P + 3) / 4, ROWS == kF32Rounded ? 3 : 4>(a, R, st);
+  if (R <= 32 / P) return launch_few<2, GPB, ROWS, (32 / P + 3) / 4, 2>(a, R, st);
   if constexpr (ROWS == kF32Rounded) {
     return hipErrorInvalidValue;
   } else {
-    // Up to three groups of 64 tile rows where 16 columns make at most one workgroup per CU: many_kernel has N / 128 workgroups for 64
-    // tile rows then, and its time is that of one, us (bf16 rows, few / many): 12288 x 4096 64 rows 28 / 89, 128 rows 57 / 90;
-    // 4096 x 4096 13 / 38.  With more columns it fills the chip: 4096 x 12288 64 rows 34 / 35, 128 rows 68 / 35.
-    if (R <= 64 / P || (R <= 3 * (64 / P) && a.ntiles <= 256))
-      return launch_few<4, GPB, ROWS, (64 / P + 3) / 4, ROWS == kF32 && VEC ? 2 : 1, VEC>(a, R, st);
+    // More than 32 tile rows: groups of 64 with either kernel.  A workgroup of few_kernel (16 columns, one to a CU) takes an eighth of
+    // the blocks of 128 k per wavefront, 2.1 us each and 2.5 us around them; one of many_kernel (128 columns, two to a CU, one for groups of 32)
+    // all of them at 1 us (1.5).  us measured (bf16 rows), few / many:  12288 x 4096, 64 rows 28 / 89, 128 rows 57 / 90, 192 rows 83 / 92;  4096 x 4096, 64 rows
+    // 13 / 38;  4096 x 12288, 64 rows 34 / 35, 128 rows 68 / 35.
+    const int64_t row_groups = (R + 64 / P - 1) / (64 / P), few = row_groups * a.ntiles, many = row_groups * ((a.ntiles + 7) / 8);
+    const double few_us = static_cast<double>((few + 255) / 256) * (2.1 * ((a.kblocks + kShares - 1) / kShares) + 2.5);
+    const double many_us = GPB < 4 ? static_cast<double>((many + 511) / 512) * a.kblocks : 1.5 * static_cast<double>((many + 255) / 256) * a.kblocks;
+    if (few_us < 1.1 * many_us && row_groups < 65536) return launch_few<4, GPB, ROWS, (64 / P + 3) / 4, ROWS == kF32 ? 2 : 1>(a, R, st);
     const int64_t grid = static_cast<int64_t>(((a.ntiles + 7) / 8 + 7) / 8 * 8) * ((R + kManyRows / P - 1) / (kManyRows / P));
     if (grid > (int64_t{1} << 30)) return hipErrorInvalidValue;
-    hipLaunchKernelGGL((many_kernel<GPB, ROWS, VEC>), dim3(static_cast<unsigned>(grid)), dim3(256), 0, st, a);
+    hipLaunchKernelGGL((many_kernel<GPB, ROWS>), dim3(static_cast<unsigned>(grid)), dim3(256), 0, st, a);
     return hipGetLastError();
   }
 }
 
-template <int GPB, int ROWS>
-hipError_t launch_vec(const Args& a, int R, hipStream_t st) {
-  return a.vec && a.K % 8 == 0 ? launch_rows<GPB, ROWS, true>(a, R, st) : launch_rows<GPB, ROWS, false>(a, R, st);
-}
-
 template <int ROWS>
 hipError_t launch_gpb(const Args& a, int gpb, int R, hipStream_t st) {
-  return gpb == 1 ? launch_vec<1, ROWS>(a, R, st) : gpb == 2 ? launch_vec<2, ROWS>(a, R, st) : launch_vec<4, ROWS>(a, R, st);
+  return gpb == 1 ? launch_rows<1, ROWS>(a, R, st) : gpb == 2 ? launch_rows<2, ROWS>(a, R, st) : launch_rows<4, ROWS>(a, R, st);
 }
 
 }  // namespace q4

@@ -46,7 +46,6 @@ struct Args {
   const void* X;
   int64_t ldx;
   int R;
-  bool vec;                  // rows and strides allow 16-byte loads
   const float* bias;         // [N], per-step table [T, N] with krow, or null
   void* Y;
   int64_t ldy;
@@ -96,42 +95,34 @@ struct Chunk {
   typedef typename std::conditional<ROWS == kBf16, bf16x8, F32x8>::type Raw;
 };
 
-// VEC: rows start on 16 bytes and K is a multiple of 8, so a chunk lies wholly before K or behind it: it is loaded without a branch
-// (from the row's last chunk where it lies behind) and zeroed when it is used.
-template <int ROWS, bool VEC>
+// It is loaded without a branch, 16 bytes at a time wherever the row starts (the hardware takes any alignment of the element type),
+// from the row's last eight values where it ends behind K; in the last block finish_chunk replaces what such a load brought.
+template <int ROWS>
 __device__ __forceinline__ void load_chunk(const Args& p, int64_t src, int k, typename Chunk<ROWS>::Raw& v) {
-  typedef typename std::conditional<ROWS == kBf16, __bf16, float>::type T;
-  const T* x = static_cast<const T*>(p.X) + src * p.ldx;
-  if constexpr (VEC) {
-    x += k < p.K ? k : p.K - 8;
-    if constexpr (ROWS == kBf16) {
-      v = *reinterpret_cast<const bf16x8*>(x);
-    } else {
-      v[0] = *reinterpret_cast<const f32x4*>(x);
-      v[1] = *reinterpret_cast<const f32x4*>(x + 4);
-    }
+  if (p.K < 8) return;                             // uniform; finish_chunk loads it
+  typedef __bf16 any8 __attribute__((ext_vector_type(8), aligned(2)));
+  typedef float any4 __attribute__((ext_vector_type(4), aligned(4)));
+  const int at = k + 8 <= p.K ? k : p.K - 8;
+  if constexpr (ROWS == kBf16) {
+    v = *reinterpret_cast<const any8*>(static_cast<const __bf16*>(p.X) + src * p.ldx + at);
   } else {
-#pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      const T t = k + e < p.K ? x[k + e] : static_cast<T>(0.f);
-      if constexpr (ROWS == kBf16) v[e] = t;
-      else v[e >> 2][e & 3] = t;
-    }
+    const float* x = static_cast<const float*>(p.X) + src * p.ldx + at;
+    v[0] = *reinterpret_cast<const any4*>(x);
+    v[1] = *reinterpret_cast<const any4*>(x + 4);
   }
 }
 
 template <int ROWS>
-__device__ __forceinline__ typename Chunk<ROWS>::Raw zero_if(bool behind, typename Chunk<ROWS>::Raw v) {
-  if constexpr (ROWS == kBf16) {
-    u32x4 t = __builtin_bit_cast(u32x4, v);
+__device__ __forceinline__ void finish_chunk(const Args& p, int64_t src, int k, typename Chunk<ROWS>::Raw& v) {
+  typedef typename std::conditional<ROWS == kBf16, __bf16, float>::type T;
+  if (k + 8 <= p.K) return;
+  const T* x = static_cast<const T*>(p.X) + src * p.ldx;
 #pragma unroll
-    for (int e = 0; e < 4; ++e) t[e] = behind ? 0u : t[e];
-    v = __builtin_bit_cast(bf16x8, t);
-  } else {
-#pragma unroll
-    for (int e = 0; e < 8; ++e) v.v[e >> 2][e & 3] = behind ? 0.f : v.v[e >> 2][e & 3];
+  for (int e = 0; e < 8; ++e) {
+    const T there = x[k + e < p.K ? k + e : p.K - 1], t = k + e < p.K ? there : static_cast<T>(0.f);
+    if constexpr (ROWS == kBf16) v[e] = t;
+    else v[e >> 2][e & 3] = t;
   }
-  return v;
 }
 
 // A row of 128 k is 256 bytes of LDS, all 64 banks: chunk c (8 k) of row v lies at c ^ (v & 15), so that a fragment read (16 rows,
@@ -209,7 +200,7 @@ __device__ __forceinline__ void finish4(const Args& p, int m, int n, f32x4 c) {
 // Weights and rows (XC chunks of 8 per lane: 4 XC rows) are requested PF blocks ahead in registers, PF being what these hold: both alike, as loads
 // return in order and waiting for a row would wait for every weight requested before it.  There is no barrier in the loop.  Tile rows
 // that no row of the call fills hold whatever was there: their sums are not used.
-template <int MT, int NT, int GPB, int ROWS, int XC, int PF, bool VEC>
+template <int MT, int NT, int GPB, int ROWS, int XC, int PF>
 __global__ __launch_bounds__(64 * kShares) void few_kernel(Args p) {
   constexpr int NW = kShares, PIECES = pieces(ROWS), kRealRows = 16 * MT / PIECES, kChunks = XC;
   constexpr int kPanel = 16 * MT * 256;
@@ -253,10 +244,9 @@ __global__ __launch_bounds__(64 * kShares) void few_kernel(Args p) {
   typedef typename Chunk<ROWS>::Raw Raw;
   Raw x[PF][kChunks];
   auto fetch_rows = [&](int b, Raw (&x)[kChunks]) {
-    if (!VEC && b >= p.kblocks) return;          // element by element, a repetition would cost
     b = b < p.kblocks ? b : p.kblocks - 1;
 #pragma unroll
-    for (int i = 0; i < kChunks; ++i) load_chunk<ROWS, VEC>(p, src[i], 128 * b + 8 * l16, x[i]);
+    for (int i = 0; i < kChunks; ++i) load_chunk<ROWS>(p, src[i], 128 * b + 8 * l16, x[i]);
   };
 #pragma unroll
   for (int i = 0; i < PF; ++i) {
@@ -269,10 +259,13 @@ __global__ __launch_bounds__(64 * kShares) void few_kernel(Args p) {
     for (int i = 0; i < PF; ++i) {
       const int b = b0 + i * NW;
       if (b >= p.kblocks) break;
+      if (128 * b + 128 > p.K) {
+#pragma unroll
+        for (int c = 0; c < kChunks; ++c) finish_chunk<ROWS>(p, src[c], 128 * b + 8 * l16, x[i][c]);
+      }
 #pragma unroll
       for (int c = 0; c < kChunks; ++c)
-        if (4 * XC <= kRealRows || (64 * c + lane) >> 4 < kRealRows)
-          put_chunk<ROWS>(panel, (64 * c + lane) >> 4, l16, VEC && 128 * b + 128 > p.K ? zero_if<ROWS>(128 * b + 8 * l16 >= p.K, x[i][c]) : x[i][c]);
+        if (4 * XC <= kRealRows || (64 * c + lane) >> 4 < kRealRows) put_chunk<ROWS>(panel, (64 * c + lane) >> 4, l16, x[i][c]);
       fetch_rows(b + PF * NW, x[i]);
       __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
       __builtin_amdgcn_wave_barrier();
@@ -340,12 +333,12 @@ __global__ __launch_bounds__(64 * kShares) void few_kernel(Args p) {
 }
 
 // ------------------------------------------------------------------------------------------------ many rows
-// 64 tile rows x 128 columns, four wavefronts of 64 x 32, two workgroups to a CU whose phases overlap (one for groups of 32
-// or odd rows, whose registers two do not leave); the rows of a block of 128 k
+// 64 tile rows x 128 columns, four wavefronts of 64 x 32, two workgroups to a CU whose phases overlap (one for groups of 32,
+// whose registers two do not leave); the rows of a block of 128 k
 // are staged through registers (where fp32 ones are split) into one of two LDS panels while the other is multiplied; weights go from memory into registers
 // two blocks ahead, as rows do, and are unpacked by the wavefronts that multiply them.
-template <int GPB, int ROWS, bool VEC>
-__global__ __launch_bounds__(256, GPB < 4 && VEC ? 2 : 1) void many_kernel(Args p) {
+template <int GPB, int ROWS>
+__global__ __launch_bounds__(256, GPB < 4 ? 2 : 1) void many_kernel(Args p) {
   constexpr int kRows = kManyRows, kPanel = kRows * 256, PIECES = pieces(ROWS), kRealRows = kRows / PIECES;
   constexpr int kChunks = (kRealRows * 16 + 255) / 256;
   __shared__ __align__(1024) unsigned char lds[2 * kPanel];
@@ -383,14 +376,17 @@ __global__ __launch_bounds__(256, GPB < 4 && VEC ? 2 : 1) void many_kernel(Args 
   int bx = 0, bw = 0, b = 0;
   auto fetch_rows = [&](Raw (&x)[kChunks]) {
 #pragma unroll
-    for (int i = 0; i < kChunks; ++i) load_chunk<ROWS, VEC>(p, src[i], 128 * bx + 8 * l16, x[i]);
+    for (int i = 0; i < kChunks; ++i) load_chunk<ROWS>(p, src[i], 128 * bx + 8 * l16, x[i]);
     bx = advance(bx);
   };
   auto put_rows = [&](int h, int block, Raw (&x)[kChunks]) {
+    if (128 * block + 128 > p.K) {
+#pragma unroll
+      for (int i = 0; i < kChunks; ++i) finish_chunk<ROWS>(p, src[i], 128 * block + 8 * l16, x[i]);
+    }
 #pragma unroll
     for (int i = 0; i < kChunks; ++i)
-      if (256 * kChunks <= 16 * kRealRows || (256 * i + t) >> 4 < kRealRows)
-        put_chunk<ROWS>(lds + h * kPanel, (256 * i + t) >> 4, l16, VEC && 128 * block + 128 > p.K ? zero_if<ROWS>(128 * block + 8 * l16 >= p.K, x[i]) : x[i]);
+      if (256 * kChunks <= 16 * kRealRows || (256 * i + t) >> 4 < kRealRows) put_chunk<ROWS>(lds + h * kPanel, (256 * i + t) >> 4, l16, x[i]);
   };
   auto fetch_weights = [&](u32x4 (&w)[2], u32x2 (&s)[2][GPB]) {
 #pragma unroll

@@ -52,7 +52,6 @@ int sdden_q4_eval(const sdden_q4* m, int32_t R, const void* X, int32_t x_type, i
   q4::Args a{};
   m->fill(a);
   a.X = X; a.ldx = x_stride; a.R = R;
-  a.vec = sdi::aligned16(X) && x_stride % (x_type == SDDEN_F32 ? 4 : 8) == 0;
   a.bias = bias;
   a.Y = Y; a.ldy = y_stride; a.y_f32 = y_type == SDDEN_F32;
   a.vec_out = sdi::aligned16(Y) && y_stride % 4 == 0;
@@ -185,15 +184,15 @@ struct Mlp4Denoiser final : sdden {
     a.R = R;
     int form = q4::kBf16;
     if (image) {
-      a.X = image; a.ldx = d; a.vec = d % 8 == 0; a.gather = true;
+      a.X = image; a.ldx = d; a.gather = true;
     } else if (R <= q4::kRoundedRows) {
-      a.X = X; a.ldx = d; a.vec = d % 4 == 0; a.gather = true;
+      a.X = X; a.ldx = d; a.gather = true;
       form = q4::kF32Rounded;
     } else {
       const int64_t chunks = static_cast<int64_t>(R) * ((d + 3) / 4);
       hipLaunchKernelGGL(gather_round_kernel, dim3(static_cast<unsigned>(std::min<int64_t>((chunks + 255) / 256, 256 * 32))), dim3(256), 0, st, X,
                          rowidx, count, Xb, d, ldx);
-      a.X = Xb; a.ldx = ldx; a.vec = true;
+      a.X = Xb; a.ldx = ldx;
     }
     a.bias = tb; a.krow = krow; a.rowidx = rowidx; a.count = count; a.silu = true;
     a.Y = H1; a.ldy = ldh; a.vec_out = true;
@@ -202,13 +201,13 @@ struct Mlp4Denoiser final : sdden {
     prof.mark(1, st);
     a = q4::Args{};
     Q2.fill(a);
-    a.X = H1; a.ldx = ldh; a.R = R; a.vec = true; a.bias = b2; a.count = count; a.silu = true; a.Y = H2; a.ldy = ldh; a.vec_out = true;
+    a.X = H1; a.ldx = ldh; a.R = R; a.bias = b2; a.count = count; a.silu = true; a.Y = H2; a.ldy = ldh; a.vec_out = true;
     prof.mark(2, st);
     SD_HIP_TRY(err, Q2.launch(a, R, q4::kBf16, st));
     prof.mark(2, st);
     a = q4::Args{};
     Q3.fill(a);
-    a.X = H2; a.ldx = ldh; a.R = R; a.vec = true; a.bias = b3; a.count = count; a.rowidx = rowidx; a.scatter = true;
+    a.X = H2; a.ldx = ldh; a.R = R; a.bias = b3; a.count = count; a.rowidx = rowidx; a.scatter = true;
     a.Y = out; a.ldy = d; a.y_f32 = true; a.vec_out = d % 4 == 0;
     prof.mark(3, st);
     SD_HIP_TRY(err, Q3.launch(a, R, q4::kBf16, st));
