@@ -138,7 +138,7 @@ const char* sdden_last_error(const sdden* den);
  * enqueued on `stream` only, nothing is allocated, synchronised or kept between calls, so any number may run at once on buffers
  * of their own, and all of them may be captured into a graph.  Matrices are row-major; a `*_stride` is the number of elements
  * between two rows.  Buffers must not overlap.  Errors: SD_ERR_* with the text in sdden_last_error(NULL), which is kept per
- * thread; nothing is enqueued then.  R = 0 is no error: no row is written, weight gradients become zero. */
+ * thread; nothing is enqueued then.  R = 0 is no error: no row is written, weight gradients become zero.  R <= 2^30. */
 #define SDDEN_F32 0
 #define SDDEN_BF16 1
 #define SDDEN_SILU 0              /* f(g) = g / (1 + exp(-g))                                     */
@@ -146,7 +146,7 @@ const char* sdden_last_error(const sdden* den);
 
 /* Layer norm:  y = (x - mean) rstd * weight + bias,  rstd = 1 / sqrt(mean((x - mean)^2) + eps), statistics in fp32.
  * x [R,d] of x_type, y [R,d] of y_type (any mix), weight and bias [d] fp32 or NULL (1 and 0), mean and rstd [R] fp32: both
- * written for the backward pass, or both NULL.  Any d > 0, any stride >= d, any alignment of the element type; 16-byte
+ * written for the backward pass, or both NULL.  Any d from 1 to 2^30, any stride >= d, any alignment of the element type; 16-byte
  * accesses are used where d, the strides and the pointers allow them. */
 int sdden_layernorm_forward(int32_t R, int32_t d, const void* x, int32_t x_type, int64_t x_stride, const float* weight,
                             const float* bias, float eps, void* y, int32_t y_type, int64_t y_stride, float* mean, float* rstd,

@@ -23,6 +23,8 @@ bool aligned_to(const void* p, size_t n) { return (reinterpret_cast<uintptr_t>(p
 size_t size_of(int32_t t) { return t == SDDEN_F32 ? 4 : 2; }
 
 // ------------------------------------------------------------------------------------------------ layer norm
+constexpr int32_t kMaxRows = 1 << 30, kMaxWidth = 1 << 30;       // of a call: sums of sizes stay within 32 bits
+
 // Threads per row and elements per thread by width: a wavefront up to 1024 columns (four rows to a workgroup), then the
 // smallest workgroup whose registers hold the row.
 enum Width { kWave, k256, k512, k1024, kLong };
@@ -113,7 +115,7 @@ int check_gated(const char* what, int32_t R, int32_t d, int32_t H, int32_t act, 
     return sdi::fail(LAYER_ERR, SD_ERR_ARG, "%s: x_stride=%lld must be a multiple of 8 from d=%d to %lld", what,
                      static_cast<long long>(x_stride), d, static_cast<long long>(kMaxStride));
   const int64_t tiles = (static_cast<int64_t>(R) + 127) / 128 * ((std::max(d, H) + 63) / 64), wtiles = (static_cast<int64_t>(d) + 127) / 128 * ((H + 127) / 128);
-  if (tiles > (1 << 28) || wtiles > (1 << 26))
+  if (R > kMaxRows || tiles > (1 << 28) || wtiles > (1 << 26))
     return sdi::fail(LAYER_ERR, SD_ERR_UNSUPPORTED, "%s: R=%d rows of d=%d, H=%d are too many for one call", what, R, d, H);
   if (!sdi::aligned16(X) || !sdi::aligned16(Wg) || !sdi::aligned16(Wu) || !sdi::aligned16(Wd))
     return sdi::fail(LAYER_ERR, SD_ERR_ARG, "%s: X and the weights must be 16-byte aligned", what);
@@ -142,6 +144,7 @@ int sdden_layernorm_forward(int32_t R, int32_t d, const void* x, int32_t x_type,
   if (!(eps >= 0.f) || std::isinf(eps)) return sdi::fail(LAYER_ERR, SD_ERR_ARG, "%s: eps must be finite and not negative", what);
   if (!aligned_to(x, size_of(x_type)) || !aligned_to(y, size_of(y_type)) || !aligned_to(weight, 4) || !aligned_to(bias, 4))
     return sdi::fail(LAYER_ERR, SD_ERR_ARG, "%s: a pointer is not aligned to its element type", what);
+  if (R > kMaxRows || d > kMaxWidth) return sdi::fail(LAYER_ERR, SD_ERR_UNSUPPORTED, "%s: R=%d and d=%d must not exceed 2^30", what, R, d);
   if (R == 0) return SD_OK;
   lnorm::Args a{};
   a.R = R; a.d = d; a.x = x; a.ldx = x_stride; a.y = y; a.ldy = y_stride; a.w = weight; a.b = bias; a.mean = mean; a.rstd = rstd; a.eps = eps;
@@ -162,6 +165,7 @@ int sdden_layernorm_backward(int32_t R, int32_t d, const void* dy, int32_t dy_ty
   if (!aligned_to(x, size_of(x_type)) || !aligned_to(dx, size_of(x_type)) || !aligned_to(dres, size_of(x_type)) ||
       !aligned_to(dy, size_of(dy_type)) || !aligned_to(weight, 4) || !aligned_to(workspace, 4))
     return sdi::fail(LAYER_ERR, SD_ERR_ARG, "%s: a pointer is not aligned to its element type", what);
+  if (R > kMaxRows || d > kMaxWidth) return sdi::fail(LAYER_ERR, SD_ERR_UNSUPPORTED, "%s: R=%d and d=%d must not exceed 2^30", what, R, d);
   const bool grads = dweight || dbias;
   if (grads && R > 0 && (!workspace || workspace_bytes < sdden_layernorm_workspace_bytes(R, d)))
     return sdi::fail(LAYER_ERR, SD_ERR_WORKSPACE, "%s: dweight and dbias need %zu bytes of workspace, got %zu", what,

@@ -45,6 +45,7 @@ int sdden_q4_eval(const sdden_q4* m, int32_t R, const void* X, int32_t x_type, i
   if ((reinterpret_cast<uintptr_t>(X) & (x_type == SDDEN_F32 ? 3 : 1)) || (reinterpret_cast<uintptr_t>(Y) & (y_type == SDDEN_F32 ? 3 : 1)) ||
       (reinterpret_cast<uintptr_t>(bias) & 3))
     return sdi::fail(Q4_ERR, SD_ERR_ARG, "%s: a pointer is not aligned to its element type", what);
+  if (R > (1 << 30)) return sdi::fail(Q4_ERR, SD_ERR_UNSUPPORTED, "%s: R=%d must not exceed 2^30", what, R);
   int device = -1;
   if (hipGetDevice(&device) != hipSuccess || device != m->device)
     return sdi::fail(Q4_ERR, SD_ERR_ARG, "%s: the matrix lies on device %d, the current device is %d", what, m->device, device);

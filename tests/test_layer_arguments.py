@@ -36,6 +36,12 @@ def test_norm_backward_refuses(kw):
     assert norm_bwd(**kw) == -1 and "sdden_layernorm_backward" in err()
 
 
+def test_sizes_beyond_the_range_are_refused():
+    big = (1 << 30) + 1
+    assert norm_fwd(R=big) == -5 and norm_fwd(d=big, xs=big, ys=big) == -5 and norm_bwd(R=big) == -5
+    assert gated_fwd(R=big) == -5 and gated_bwd(R=big) == -5
+
+
 def test_norm_backward_needs_its_workspace():
     need = B.sdden_layernorm_workspace_bytes(4, 64)
     assert need > 0 and B.sdden_layernorm_workspace_bytes(0, 64) == 0 and B.sdden_layernorm_workspace_bytes(4, 0) == 0
