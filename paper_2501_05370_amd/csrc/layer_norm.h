@@ -28,7 +28,6 @@ struct Args {
   float* mean;                  // forward: out or null; backward: in
   float* rstd;
   float eps;
-  bool keep;                    // the output is small enough to stay in the caches
   float* partial;               // backward: [2, grid, d] or null
   const int32_t* count;         // forward: rows that count, at most R (device; null: R)
 };
@@ -53,9 +52,10 @@ __device__ __forceinline__ void load(const T* p, float (&v)[V]) {
   for (int e = 0; e < V; ++e) v[e] = r[e];
 }
 
-// keep: into the caches, for the kernel that reads it next; else past them.
-template <int V, typename T>
-__device__ __forceinline__ void store(T* p, const float (&v)[V], bool keep) {
+// KEEP: into the caches, for the kernel that reads it next; else past them.  (A template: the compiler would make one ordinary
+// store of the two sides of a branch.)
+template <int V, bool KEEP, typename T>
+__device__ __forceinline__ void store(T* p, const float (&v)[V]) {
   typedef typename Raw<V, T>::vec vec;
   if constexpr (V == 1) {
     *p = static_cast<T>(v[0]);
@@ -63,7 +63,7 @@ __device__ __forceinline__ void store(T* p, const float (&v)[V], bool keep) {
     vec t;
 #pragma unroll
     for (int e = 0; e < V; ++e) t[e] = static_cast<T>(v[e]);
-    if (keep) *reinterpret_cast<vec*>(p) = t;
+    if constexpr (KEEP) *reinterpret_cast<vec*>(p) = t;
     else __builtin_nontemporal_store(t, reinterpret_cast<vec*>(p));
   }
 }
@@ -91,7 +91,7 @@ __device__ __forceinline__ void row_sum2(float& a, float& b, float2 (&red)[2][16
 constexpr int threads_of(int tpr) { return tpr < 256 ? 256 : tpr; }
 
 // Columns of a thread: chunk c of V elements starts at (c * TPR + lane of the row) * V.
-template <int TPR, int E, int V, typename TX, typename TY>
+template <int TPR, int E, int V, bool KEEP, typename TX, typename TY>
 __global__ __launch_bounds__(threads_of(TPR)) void forward_kernel(Args p) {
   if (p.count) p.R = *p.count < p.R ? *p.count : p.R;
   constexpr int C = E / V, RPB = threads_of(TPR) / TPR;
@@ -158,7 +158,7 @@ __global__ __launch_bounds__(threads_of(TPR)) void forward_kernel(Args p) {
       if (col < p.d) {
 #pragma unroll
         for (int e = 0; e < V; ++e) v[c][e] = v[c][e] * rstd * w[c][e] + b[c][e];
-        store<V>(y + col, v[c], p.keep);
+        store<V, KEEP>(y + col, v[c]);
       }
     }
   }
@@ -195,7 +195,7 @@ __global__ __launch_bounds__(1024) void forward_long_kernel(Args p) {
 }
 
 // TY is dy's type, TX that of x, dres and dx.
-template <int TPR, int E, int V, typename TX, typename TY>
+template <int TPR, int E, int V, bool KEEP, typename TX, typename TY>
 __global__ __launch_bounds__(threads_of(TPR)) void backward_kernel(Args p) {
   constexpr int C = E / V, RPB = threads_of(TPR) / TPR;
   __shared__ float2 red[2][16];
@@ -257,7 +257,7 @@ __global__ __launch_bounds__(threads_of(TPR)) void backward_kernel(Args p) {
 #pragma unroll
           for (int e = 0; e < V; ++e) o[e] += add[c][e];
         }
-        store<V>(dx + col, o, p.keep);
+        store<V, KEEP>(dx + col, o);
       }
     }
   }

@@ -43,30 +43,43 @@ int partial_rows(int R, int d) {
 // the caches 58 + 125.
 constexpr int64_t kKeepBytes = int64_t{32} << 20;
 
-template <int V, typename TX, typename TY>
-void norm_forward(const lnorm::Args& a, hipStream_t st) {
+template <int V, bool KEEP, typename TX, typename TY>
+void norm_forward_kept(const lnorm::Args& a, hipStream_t st) {
   const int R = a.R;
   switch (width_of(a.d)) {
-    case kWave: hipLaunchKernelGGL((lnorm::forward_kernel<64, 16, V, TX, TY>), dim3(std::min((R + 3) / 4, 2048)), dim3(256), 0, st, a); break;
-    case k256: hipLaunchKernelGGL((lnorm::forward_kernel<256, 16, V, TX, TY>), dim3(std::min(R, 2048)), dim3(256), 0, st, a); break;
-    case k512: hipLaunchKernelGGL((lnorm::forward_kernel<512, 24, V, TX, TY>), dim3(std::min(R, 1024)), dim3(512), 0, st, a); break;
-    case k1024: hipLaunchKernelGGL((lnorm::forward_kernel<1024, 16, V, TX, TY>), dim3(std::min(R, 512)), dim3(1024), 0, st, a); break;
+    case kWave: hipLaunchKernelGGL((lnorm::forward_kernel<64, 16, V, KEEP, TX, TY>), dim3(std::min((R + 3) / 4, 2048)), dim3(256), 0, st, a); break;
+    case k256: hipLaunchKernelGGL((lnorm::forward_kernel<256, 16, V, KEEP, TX, TY>), dim3(std::min(R, 2048)), dim3(256), 0, st, a); break;
+    case k512: hipLaunchKernelGGL((lnorm::forward_kernel<512, 24, V, KEEP, TX, TY>), dim3(std::min(R, 1024)), dim3(512), 0, st, a); break;
+    case k1024: hipLaunchKernelGGL((lnorm::forward_kernel<1024, 16, V, KEEP, TX, TY>), dim3(std::min(R, 512)), dim3(1024), 0, st, a); break;
     default: hipLaunchKernelGGL((lnorm::forward_long_kernel<TX, TY>), dim3(std::min(R, 512)), dim3(1024), 0, st, a); break;
   }
 }
 
-template <int V, typename TX, typename TY>
-void norm_backward(const lnorm::Args& a, int P, hipStream_t st) {
+template <int V, bool KEEP, typename TX, typename TY>
+void norm_backward_kept(const lnorm::Args& a, int P, hipStream_t st) {
   switch (width_of(a.d)) {
-    case kWave: hipLaunchKernelGGL((lnorm::backward_kernel<64, 16, V, TX, TY>), dim3(P), dim3(256), 0, st, a); break;
-    case k256: hipLaunchKernelGGL((lnorm::backward_kernel<256, 16, V, TX, TY>), dim3(P), dim3(256), 0, st, a); break;
-    case k512: hipLaunchKernelGGL((lnorm::backward_kernel<512, 24, V, TX, TY>), dim3(P), dim3(512), 0, st, a); break;
-    case k1024: hipLaunchKernelGGL((lnorm::backward_kernel<1024, 16, V, TX, TY>), dim3(P), dim3(1024), 0, st, a); break;
+    case kWave: hipLaunchKernelGGL((lnorm::backward_kernel<64, 16, V, KEEP, TX, TY>), dim3(P), dim3(256), 0, st, a); break;
+    case k256: hipLaunchKernelGGL((lnorm::backward_kernel<256, 16, V, KEEP, TX, TY>), dim3(P), dim3(256), 0, st, a); break;
+    case k512: hipLaunchKernelGGL((lnorm::backward_kernel<512, 24, V, KEEP, TX, TY>), dim3(P), dim3(512), 0, st, a); break;
+    case k1024: hipLaunchKernelGGL((lnorm::backward_kernel<1024, 16, V, KEEP, TX, TY>), dim3(P), dim3(1024), 0, st, a); break;
     default:
       hipLaunchKernelGGL((lnorm::backward_long_kernel<TX, TY>), dim3(std::min(a.R, 512)), dim3(1024), 0, st, a);
       if (a.partial) hipLaunchKernelGGL((lnorm::long_partials_kernel<TX, TY>), dim3((a.d + 255) / 256, P), dim3(256), 0, st, a);
       break;
   }
+}
+
+// (element by element, or long: always kept)
+template <int V, typename TX, typename TY>
+void norm_forward(const lnorm::Args& a, hipStream_t st) {
+  if (V > 1 && static_cast<int64_t>(a.R) * a.d * static_cast<int64_t>(sizeof(TY)) > kKeepBytes) norm_forward_kept<V, V == 1, TX, TY>(a, st);
+  else norm_forward_kept<V, true, TX, TY>(a, st);
+}
+
+template <int V, typename TX, typename TY>
+void norm_backward(const lnorm::Args& a, int P, hipStream_t st) {
+  if (V > 1 && static_cast<int64_t>(a.R) * a.d * static_cast<int64_t>(sizeof(TX)) > kKeepBytes) norm_backward_kept<V, V == 1, TX, TY>(a, P, st);
+  else norm_backward_kept<V, true, TX, TY>(a, P, st);
 }
 
 // Calls `go` with the vector width and the two types of the call as template arguments.
@@ -148,7 +161,6 @@ int sdden_layernorm_forward(int32_t R, int32_t d, const void* x, int32_t x_type,
   if (R == 0) return SD_OK;
   lnorm::Args a{};
   a.R = R; a.d = d; a.x = x; a.ldx = x_stride; a.y = y; a.ldy = y_stride; a.w = weight; a.b = bias; a.mean = mean; a.rstd = rstd; a.eps = eps;
-  a.keep = static_cast<int64_t>(R) * d * static_cast<int64_t>(size_of(y_type)) <= kKeepBytes;
   const int vec = vector_width(d, x_type, y_type, {x_stride, y_stride}, {x, y, weight, bias});
   by_type(vec, x_type, y_type, [&](auto v, auto tx, auto ty) { norm_forward<decltype(v)::value, decltype(tx), decltype(ty)>(a, static_cast<hipStream_t>(stream)); });
   return done(what, hipGetLastError());
@@ -174,7 +186,6 @@ int sdden_layernorm_backward(int32_t R, int32_t d, const void* dy, int32_t dy_ty
   a.R = R; a.d = d; a.x = x; a.ldx = x_stride; a.dy = dy; a.lddy = dy_stride; a.dres = dres; a.lddres = dres ? dres_stride : 0;
   a.y = dx; a.ldy = dx_stride; a.w = weight; a.mean = const_cast<float*>(mean); a.rstd = const_cast<float*>(rstd);
   a.partial = grads ? static_cast<float*>(workspace) : nullptr;
-  a.keep = static_cast<int64_t>(R) * d * static_cast<int64_t>(size_of(x_type)) <= kKeepBytes;
   hipStream_t st = static_cast<hipStream_t>(stream);
   const int P = R > 0 ? partial_rows(R, d) : 0;
   if (R > 0) {
@@ -339,7 +350,7 @@ struct GatedDenoiser final : sdden {
                        table, rowidx, krow, count, h, d);
     for (int l = 0; l < blocks; ++l) {
       lnorm::Args a{};
-      a.R = R; a.d = d; a.x = h; a.ldx = d; a.y = n; a.ldy = d; a.eps = eps; a.count = count; a.keep = true;
+      a.R = R; a.d = d; a.x = h; a.ldx = d; a.y = n; a.ldy = d; a.eps = eps; a.count = count;
       a.w = nw + static_cast<int64_t>(l) * d;
       a.b = nb + static_cast<int64_t>(l) * d;
       prof.mark(1, st);
