@@ -15,6 +15,8 @@
 //            k = 0..3 and 8..11 of a step (then 4..7 and 12..15, ...), f gives those eight rows different segments modulo
 //            256 bytes:  HB = 128: f = (k & 3) | (k >> 1 & 4);  HB = 64 (two rows per 256 bytes): f = (k >> 1 & 1) | (k >> 2 & 2);
 //            HB = 32 (four rows): f = k >> 3 & 1
+// Every kernel below sums an output over k in one chain of 16x16x32 instructions and in order, whatever its tile: a row's result
+// does not depend on how many rows a call has (tested; the instruction set does not promise it).
 // Ends: rows i past the end repeat the last one (their outputs are not stored, and an output takes nothing from another row);
 // k past the end is loaded from 16 zero bytes in both operands, so whatever lies there (NaN included) stays out of the sums.
 #pragma once
@@ -359,7 +361,10 @@ __global__ __launch_bounds__(256) void tile_kernel(Args a) {
 // next (12 younger loads may be outstanding), so that no register is in flight where the compiler could move it.  The builtin for
 // the transposing read would wait for every load in flight.  The block sets m0 (the loads' place in LDS) itself; nothing behind it
 // reads an older value: the builtin loads, which set their own, all come before the loop.
-// 128 KiB of LDS, one workgroup per CU.
+// 128 KiB of LDS, one workgroup per CU.  Bound by the clock that the power allows (the loop is that of mlp_gemm_pp.h) and, where an
+// epilogue moves fp32 gates, by HBM while the matrix cores wait.  PFLOP/s: 7680 rows, d = 12288, H = 4096 first products 1.38, last
+// 1.45; 8192 rows, d = 4096, H = 11008 with gates kept (0.9 GB written) 1.24, last 1.38, dA with the gates' gradients (0.7 GB read,
+// 0.4 written) 0.86, dX 1.40, the three weight gradients in one launch 1.20 (2064 tiles: the ninth round of 256 is nearly empty).
 template <int OFF, bool LD, int W>
 __device__ __forceinline__ void phase_along8(u32x4 (&f)[8], uint32_t ad0, uint32_t ad1, const void* g0, const void* g1, uint32_t m0, uint32_t m1) {
 #define LG_READS                                                                                                        \

@@ -6,6 +6,8 @@
 // Bound by HBM: each row is read once and kept in registers (E elements per thread of the TPR threads that share a row), so the
 // variance is the two-pass one, the sum of (x - mean)^2 around the finished mean, at no further traffic; everything between the
 // loads and the stores is fp32.  Rows longer than the widest register form are walked in three passes, out of L2.
+// Measured: 7680 fp32 rows of 12288 to bf16 121 us (4.7 TB/s; a large copy reaches 4.8), 16384 bf16 rows of 4096 forward 55 us
+// (4.8 TB/s), backward with dres 101 us (5.3 TB/s, part of x still cached) and 7 us for the weights' gradients; one row 4 us.
 // The weights' gradients need a sum over all rows: a workgroup walks rows blockIdx, blockIdx + grid, ... with its columns'
 // sums in registers and leaves one partial row; reduce_partials_kernel adds those up in a fixed order (no atomics: the
 // same bits every time).
