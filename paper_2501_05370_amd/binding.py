@@ -484,6 +484,7 @@ class Denoiser:
 # the host, so the checks ask each tensor once and build their messages only when one fails.
 _F32, _BF16 = torch.float32, torch.bfloat16
 _LAYER_TYPES = {_F32: SDDEN_F32, _BF16: SDDEN_BF16}
+_MAX_ROWS = 1 << 30
 
 
 def _rows(t: Optional[torch.Tensor], name: str, shape=None, only=None, allow_none: bool = False):
@@ -499,6 +500,8 @@ def _rows(t: Optional[torch.Tensor], name: str, shape=None, only=None, allow_non
     if shape is not None and dims != shape:
         raise SDError(f"{name}: need shape {tuple(shape)}, got {tuple(dims)}")
     R, d = dims
+    if R > _MAX_ROWS or d > _MAX_ROWS:               # the library's sizes are 32 bits wide
+        raise SDError(f"{name}: {R} rows of {d} are more than one call takes (2^30)")
     stride, inner = t.stride()
     if inner != 1 and d > 1:
         raise SDError(f"{name}: the elements of a row must be contiguous, got strides {t.stride()}")

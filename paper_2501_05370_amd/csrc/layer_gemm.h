@@ -265,7 +265,7 @@ __global__ __launch_bounds__(256) void tile_kernel(Args a) {
   const int m0 = tm * 2 * HB, n0 = tn * (EPI == kGate ? HB : 2 * HB);
   const int slices = (p.K + 63) / 64, nk = slices * p.ranges;
 
-  // Wavefront w fills one panel per stage: A0, A1, B0, B1 (eight loads of 1 KiB).
+  // Wavefront w fills one half panel per stage: A0, A1, B0, B1 (HB / 8 loads of 1 KiB).
   const bool is_b = wave >= 2;
   const int64_t ld = is_b ? p.ldb : p.lda;
   int i0, valid;

@@ -112,3 +112,12 @@ def test_two_steps_at_once_on_two_streams():
     torch.cuda.synchronize()
     for s, want in zip(states, alone):
         assert all(torch.equal(s[k], t) for k, t in zip(outs, want))
+
+
+def test_more_rows_than_a_call_takes_are_refused():
+    """The library's sizes are 32 bits wide: more must not be taken for what is left of them."""
+    x = torch.empty((1 << 30) + 1, 1, dtype=BF, device="cuda")
+    with pytest.raises(B.SDError, match="2\\^30"):
+        B.sdden_layernorm_forward(x, None, None, 1e-5, x)
+    with pytest.raises(B.SDError, match="2\\^30"):
+        B.sdden_layernorm_forward(x.view(1, -1), None, None, 1e-5, x.view(1, -1))
