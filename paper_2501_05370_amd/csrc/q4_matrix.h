@@ -29,6 +29,12 @@ template <int GPB, int ROWS>
 hipError_t launch_rows(const Args& a, int R, hipStream_t st) {
   constexpr int P = pieces(ROWS);
   if (R <= 4) return launch_few<1, GPB, ROWS, 1, 4>(a, R, st);
+  // Rows are staged four at a time and lane: tiles of 16 and 32 rows have a form for their lower half.  us with / without, 12288 x 4096:
+  // 8 rows 8.8 / 11.7, 19 rows 14.2 / 16.3; 4096 x 12288 (groups of 64): 8 rows 12.6 / 15.6, 19 rows 17.3 / 18.9
+  if constexpr (P == 1) {
+    if (R <= 8) return launch_few<1, GPB, ROWS, 2, 4>(a, R, st);
+    if (R > 16 && R <= 24) return launch_few<2, GPB, ROWS, 6, 2>(a, R, st);
+  }
   if (R <= 16 / P) return launch_few<1, GPB, ROWS, (16 / P + 3) / 4, ROWS == kF32Rounded ? 3 : 4>(a, R, st);
   if (R <= 32 / P) return launch_few<2, GPB, ROWS, (32 / P + 3) / 4, 2>(a, R, st);
   if constexpr (ROWS == kF32Rounded) {

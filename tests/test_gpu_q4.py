@@ -137,3 +137,18 @@ def test_streams_and_graphs_share_a_matrix():
             g.replay()
         torch.cuda.synchronize()
         assert all(torch.equal(a, b) for a, b in zip(ys, want))
+
+
+@pytest.mark.parametrize("K,N,group,t", [(1100, 200, 32, BF), (1100, 200, 128, F32), (515, 8208, 64, BF), (515, 8208, 128, F32)])
+def test_a_row_does_not_depend_on_the_call(K, N, group, t):
+    """Row counts at the edges of every kernel and of its rows per lane: the same bits as in one large call."""
+    rng = np.random.default_rng(5)
+    q, scale, _, _ = matrix(rng, N, K, group)
+    m = B.Q4Matrix.sdden_q4_create(q, scale, K, group)
+    x = torch.randn(600, K, device="cuda").to(t)
+    whole = torch.empty(600, N, device="cuda")
+    m.sdden_q4_eval(x, whole)
+    for R in (1, 4, 5, 6, 8, 9, 10, 11, 16, 17, 21, 22, 24, 25, 32, 33, 42, 43, 64, 65, 128, 129, 192, 193, 300):
+        y = torch.full((R, N), float("nan"), device="cuda")
+        m.sdden_q4_eval(x[:R], y)
+        assert torch.equal(y, whole[:R]), R
