@@ -13,7 +13,7 @@ constexpr int kRoundedRows = 32;      // most rows of a call with kF32Rounded
 template <int MT, int GPB, int ROWS, int XC, int PF>
 hipError_t launch_few(const Args& a, int R, hipStream_t st) {
   // 32 columns a workgroup where that still gives every CU one: the rows' panel is written once for both.  us, 32 / 16 columns, 4096 x 12288:
-  // 19 rows, groups of 64 19.0 / 22.5; one row, groups of 32 15.8 / 12.6 (registers for one workgroup per CU)
+  // 32 staged rows, groups of 64 19.0 / 22.5; one row, groups of 32 15.8 / 12.6 (registers for one workgroup per CU)
   if constexpr (MT <= 2 && GPB <= 2) {
     if (a.ntiles >= 512) {                   // (one group of rows: see launch_rows)
       hipLaunchKernelGGL((few_kernel<MT, 2, GPB, ROWS, XC, PF>), dim3((a.ntiles + 1) / 2), dim3(64 * kShares), 0, st, a);
@@ -29,7 +29,8 @@ template <int GPB, int ROWS>
 hipError_t launch_rows(const Args& a, int R, hipStream_t st) {
   constexpr int P = pieces(ROWS);
   if (R <= 4) return launch_few<1, GPB, ROWS, 1, 4>(a, R, st);
-  // Rows are staged four at a time and lane: tiles of 16 and 32 rows have a form for their lower half.  us with / without, 12288 x 4096:
+  // A lane stages one row in four: a tile of 16 rows has a form that stages 8, one of 32 a form that stages 24.  us with / without (the
+  // whole tile's form, which takes the same time for any rows of it), bf16, 12288 x 4096 (groups of 128):
   // 8 rows 8.8 / 11.7, 19 rows 14.2 / 16.3; 4096 x 12288 (groups of 64): 8 rows 12.6 / 15.6, 19 rows 17.3 / 18.9
   if constexpr (P == 1) {
     if (R <= 8) return launch_few<1, GPB, ROWS, 2, 4>(a, R, st);
