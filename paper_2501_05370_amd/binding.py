@@ -395,6 +395,7 @@ class Denoiser:
         b1, b2, b3 = (_host(v, np.float32) for v in (p.b1, p.b2, p.b3))
         if W1.shape != (p.d + p.E, p.H) or W2.shape != (p.H, p.H) or W3.shape != (p.H, p.d):
             raise SDError(f"sdden_mlp4_create: weights of shapes {W1.shape}, {W2.shape}, {W3.shape} do not fit d={p.d}, H={p.H}, E={p.E}")
+        _check_group(group, "sdden_mlp4_create")
         h = c_void_p()
         rc = lib.sdden_mlp4_create(p.d, p.H, p.E, group, W1.ctypes.data, b1.ctypes.data, W2.ctypes.data, b2.ctypes.data,
                                    W3.ctypes.data, b3.ctypes.data, T, Rmax, ctypes.byref(h))
@@ -538,6 +539,12 @@ def _layer_check(lib, rc: int, what: str):
         raise SDError(f"{what} failed ({rc}): {lib.sdden_last_error(None).decode()}")
 
 
+def _check_group(group: int, what: str):
+    """ctypes would hand on the low 32 bits of a larger number: another group than the scales were laid out for."""
+    if not 0 < group < 1 << 31:
+        raise SDError(f"{what}: group={group} must be positive and below 2^31")
+
+
 def sdden_layernorm_workspace_bytes(R: int, d: int) -> int:
     return int(load_library().sdden_layernorm_workspace_bytes(R, d))
 
@@ -631,6 +638,7 @@ class Q4Matrix:
                 or q.shape[1] != (K + 1) // 2 or scale.shape != (q.shape[0], -(-K // group)):
             raise SDError(f"sdden_q4_create: need uint8 [N, ceil(K/2)] and 16-bit [N, ceil(K/group)] for K={K}, group={group}, got "
                           f"{q.dtype} {q.shape} and {scale.dtype} {scale.shape}")
+        _check_group(group, "sdden_q4_create")
         h = c_void_p()
         rc = lib.sdden_q4_create(q.shape[0], K, group, q.ctypes.data, scale.ctypes.data, ctypes.byref(h))
         _layer_check(lib, rc, "sdden_q4_create")

@@ -81,7 +81,7 @@ struct sdden_q4 {
     ntiles = (N + 15) / 16;
     kblocks = (K + 127) / 128;
     const size_t blocks = static_cast<size_t>(ntiles) * kblocks, qbytes = static_cast<size_t>(N) * ((K + 1) / 2);
-    const size_t sbytes = static_cast<size_t>(N) * ((K + group - 1) / group) * 2;
+    const size_t sbytes = static_cast<size_t>(N) * q4::groups_of(K, group) * 2;
     uint8_t* dq = nullptr;
     uint16_t* ds = nullptr;
     hipError_t e = hipGetDevice(&device);

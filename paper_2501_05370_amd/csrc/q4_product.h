@@ -28,6 +28,7 @@
 
 #include "layer_gemm.h"
 #include "lds_ring.h"
+#include "q4_shape.h"
 
 namespace q4 {
 
@@ -524,7 +525,7 @@ __global__ __launch_bounds__(256) void pack_kernel(const uint8_t* __restrict__ q
   // lq is the group within the block where it has one
   if (lq < gpb) {
     const int k = 128 * b + (128 / gpb) * lq;
-    const int64_t groups = (K + group - 1) / group;
+    const int64_t groups = groups_of(K, group);
     S[(block * gpb + lq) * 16 + l16] = n < N && k < K ? s[n * groups + k / group] : static_cast<uint16_t>(0);
   }
 }

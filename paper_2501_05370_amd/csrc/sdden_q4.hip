@@ -89,7 +89,7 @@ float bf16_round(float x) {          // to nearest even; finite values only
 // W [K, N] bf16 (row = input) -> q [N, ceil(K/2)], scale [N, ceil(K/group)]: scale = bf16(max |w| / 7) over the group's inputs,
 // q = round(w / scale) + 8 within 0..15; a group of zeros has scale 0 and q = 8.
 void quantize(const uint16_t* W, int K, int N, int group, std::vector<uint8_t>& q, std::vector<uint16_t>& scale) {
-  const int groups = (K + group - 1) / group;
+  const int groups = q4::groups_of(K, group);
   const size_t rowbytes = (static_cast<size_t>(K) + 1) / 2;
   q.assign(static_cast<size_t>(N) * rowbytes, 0);
   scale.assign(static_cast<size_t>(N) * groups, 0);
