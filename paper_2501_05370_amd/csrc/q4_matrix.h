@@ -2,6 +2,8 @@
 #pragma once
 #include <hip/hip_runtime.h>
 
+#include <algorithm>
+
 #include "q4_product.h"
 
 namespace q4 {
@@ -49,10 +51,15 @@ hipError_t launch_rows(const Args& a, int R, hipStream_t st) {
     const double few_us = static_cast<double>((few + 255) / 256) * (2.1 * ((a.kblocks + kShares - 1) / kShares) + 2.5);
     const double many_us = GPB < 4 ? static_cast<double>((many + 511) / 512) * a.kblocks : 1.5 * static_cast<double>((many + 255) / 256) * a.kblocks;
     if (few_us < 1.1 * many_us && row_groups < 65536) return launch_few<4, GPB, ROWS, (64 / P + 3) / 4, ROWS == kF32 ? 2 : 1>(a, R, st);
-    const int64_t grid = static_cast<int64_t>(((a.ntiles + 7) / 8 + 7) / 8 * 8) * ((R + kManyRows / P - 1) / (kManyRows / P));
-    if (grid > (int64_t{1} << 30)) return hipErrorInvalidValue;
-    hipLaunchKernelGGL((many_kernel<GPB, ROWS>), dim3(static_cast<unsigned>(grid)), dim3(256), 0, st, a);
-    return hipGetLastError();
+    Args part = a;
+    const int64_t most = many_groups(a.ntiles);
+    for (int64_t g = 0; g < row_groups; g += most) {
+      part.group0 = static_cast<int>(g);
+      const int64_t groups = std::min(most, row_groups - g);
+      hipLaunchKernelGGL((many_kernel<GPB, ROWS>), dim3(static_cast<unsigned>(many_columns(a.ntiles) * groups)), dim3(256), 0, st, part);
+      if (const hipError_t e = hipGetLastError(); e != hipSuccess) return e;
+    }
+    return hipSuccess;
   }
 }
 
@@ -92,7 +99,7 @@ struct sdden_q4 {
     if (e == hipSuccess) e = hipMemcpy(dq, q, qbytes, hipMemcpyHostToDevice);
     if (e == hipSuccess) e = hipMemcpy(ds, scale, sbytes, hipMemcpyHostToDevice);
     if (e == hipSuccess) {
-      hipLaunchKernelGGL(q4::pack_kernel, dim3(static_cast<unsigned>((blocks * 64 + 255) / 256)), dim3(256), 0, nullptr, dq, ds, N, K, group,
+      hipLaunchKernelGGL(q4::pack_kernel, dim3(q4::pack_grid(static_cast<int64_t>(blocks))), dim3(256), 0, nullptr, dq, ds, N, K, group,
                          gpb, ntiles, kblocks, W, S);
       e = hipGetLastError();
     }

@@ -50,6 +50,7 @@ struct Args {
   const void* X;
   int64_t ldx;
   int R;
+  int group0;                // many_kernel: the launch's first group of rows
   const float* bias;         // [N], per-step table [T, N] with krow, or null
   void* Y;
   int64_t ldy;
@@ -351,7 +352,7 @@ __global__ __launch_bounds__(256, GPB < 4 ? 2 : 1) void many_kernel(Args p) {
   const int M = p.count ? (*p.count < p.R ? *p.count : p.R) : p.R;
   // the row groups of 128 columns run on the same XCD, one after the other: its L2 serves the weights to all but the first
   const int coltiles = (p.ntiles + 7) / 8, groups = gridDim.x / ((coltiles + 7) / 8 * 8), id = blockIdx.x >> 3;
-  const int ct = (id / groups) * 8 + (blockIdx.x & 7), group = id % groups;
+  const int ct = (id / groups) * 8 + (blockIdx.x & 7), group = p.group0 + id % groups;
   const int row0 = group * kRealRows, rows = M - row0 < kRealRows ? M - row0 : kRealRows;
   if (ct >= coltiles || rows <= 0) return;
   typedef typename Chunk<ROWS>::Raw Raw;
@@ -496,37 +497,36 @@ __global__ __launch_bounds__(256, GPB < 4 ? 2 : 1) void many_kernel(Args p) {
 }
 
 // ------------------------------------------------------------------------------------------------ layout
-// q [N, ceil(K / 2)] (even k in the low half of a byte) and s [N, ceil(K / group)] -> W and S above; one thread per 16 bytes of W.
+// q [N, ceil(K / 2)] (even k in the low half of a byte) and s [N, ceil(K / group)] -> W and S above; one thread at a time per 16 bytes of W.
 __global__ __launch_bounds__(256) void pack_kernel(const uint8_t* __restrict__ q, const uint16_t* __restrict__ s, int N, int K, int group,
                                                    int gpb, int ntiles, int kblocks, u32x4* __restrict__ W, uint16_t* __restrict__ S) {
-  const int64_t id = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x;
-  if (id >= static_cast<int64_t>(ntiles) * kblocks * 64) return;
-  const int lane = static_cast<int>(id & 63), l16 = lane & 15, lq = lane >> 4;
-  const int64_t block = id >> 6;
-  const int nt = static_cast<int>(block / kblocks), b = static_cast<int>(block % kblocks);
-  const int n = nt * 16 + l16;
-  const int64_t rowbytes = (K + 1) / 2;
-  u32x4 out;
+  const int64_t rowbytes = (K + 1) / 2, groups = groups_of(K, group), total = static_cast<int64_t>(ntiles) * kblocks * 64;
+  for (int64_t id = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x; id < total; id += static_cast<int64_t>(gridDim.x) * 256) {
+    const int lane = static_cast<int>(id & 63), l16 = lane & 15, lq = lane >> 4;
+    const int64_t block = id >> 6;
+    const int nt = static_cast<int>(block / kblocks), b = static_cast<int>(block % kblocks);
+    const int n = nt * 16 + l16;
+    u32x4 out;
 #pragma unroll
-  for (int j = 0; j < 4; ++j) {
-    uint32_t v = 0;
-    for (int e = 0; e < 8; ++e) {
-      const int k = 128 * b + 32 * j + 8 * lq + e;
-      uint32_t x = 8;
-      if (n < N && k < K) {
-        const uint8_t byte = q[n * rowbytes + (k >> 1)];
-        x = k & 1 ? byte >> 4 : byte & 15;
+    for (int j = 0; j < 4; ++j) {
+      uint32_t v = 0;
+      for (int e = 0; e < 8; ++e) {
+        const int k = 128 * b + 32 * j + 8 * lq + e;
+        uint32_t x = 8;
+        if (n < N && k < K) {
+          const uint8_t byte = q[n * rowbytes + (k >> 1)];
+          x = k & 1 ? byte >> 4 : byte & 15;
+        }
+        v |= x << (8 * (e & 3) + 4 * (e >> 2));
       }
-      v |= x << (8 * (e & 3) + 4 * (e >> 2));
+      out[j] = v;
     }
-    out[j] = v;
-  }
-  W[id] = out;
-  // lq is the group within the block where it has one
-  if (lq < gpb) {
-    const int k = 128 * b + (128 / gpb) * lq;
-    const int64_t groups = groups_of(K, group);
-    S[(block * gpb + lq) * 16 + l16] = n < N && k < K ? s[n * groups + k / group] : static_cast<uint16_t>(0);
+    W[id] = out;
+    // lq is the group within the block where it has one
+    if (lq < gpb) {
+      const int k = 128 * b + (128 / gpb) * lq;
+      S[(block * gpb + lq) * 16 + l16] = n < N && k < K ? s[n * groups + k / group] : static_cast<uint16_t>(0);
+    }
   }
 }
 

@@ -1,4 +1,4 @@
-"""4-bit matrices at the ends of what a call takes: the largest groups."""
+"""4-bit matrices at the ends of what a call takes: the largest groups, more rows than one launch holds."""
 import numpy as np
 import pytest
 import torch
@@ -24,3 +24,23 @@ def test_a_group_longer_than_any_row():
         got.append(y)
         m.close()
     assert torch.equal(got[0], got[1]) and torch.equal(got[0], got[2])
+
+
+@pytest.mark.parametrize("K,N,tx,R", [(3, 5, F32, 45_000_000), (1, 8, BF, (1 << 27) + 77)])
+def test_more_rows_than_a_launch_holds(K, N, tx, R):
+    """2^24 workgroups of 256 threads hold 44 040 171 fp32 rows of up to 1024 columns, or 2^27 bf16 ones: what is more goes into
+    another launch.  The rows repeat, so every one of them must have the first ones' results."""
+    rng = np.random.default_rng(3)
+    q = rng.integers(0, 256, size=(N, (K + 1) // 2), dtype=np.uint8)
+    s = torch.from_numpy(rng.uniform(0.01, 0.1, size=(N, 1))).to(BF).view(torch.int16).numpy()
+    m = B.Q4Matrix.sdden_q4_create(q, s, K, 32)
+    period = 1009
+    some = torch.from_numpy(rng.standard_normal((period, K))).to(tx).cuda()
+    x = some.repeat(-(-R // period), 1)[:R]
+    want, y = torch.empty(period, N, dtype=BF, device="cuda"), torch.full((R + 1, N), float("nan"), dtype=BF, device="cuda")
+    m.sdden_q4_eval(some, want)
+    m.sdden_q4_eval(x, y[:R])
+    whole = R // period * period
+    assert torch.equal(y[:whole].view(-1, period, N), want.expand(whole // period, period, N))
+    assert torch.equal(y[whole:R], want[:R - whole]) and y[R].isnan().all()
+    m.close()
