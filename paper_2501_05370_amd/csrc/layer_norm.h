@@ -339,31 +339,39 @@ __global__ __launch_bounds__(256) void long_partials_kernel(Args p) {
   p.partial[static_cast<int64_t>(gridDim.y + blockIdx.y) * p.d + c] = sb;
 }
 
-// dw[0..d) and db[0..d): sums of the P partial rows; 32 columns x 32 shares of the rows per workgroup, eight loads of a share in
-// flight.  Bound by latency: 1024 partial rows of 4096 (33 MB, just written) in 7 us.
+// dw[0..d) and db[0..d): sums of the P partial rows; 32 columns x 32 shares of the rows at a time per workgroup, eight loads of a
+// share in flight.  Bound by latency: 1024 partial rows of 4096 (33 MB, just written) in 7 us.
+constexpr int kReduceCols = 32;
+// Workgroups of 1024 threads for d columns; a grid has to stay below 2^32 threads, so they walk the columns of wide rows.
+inline unsigned reduce_grid(int d) { return d < kReduceCols << 20 ? (d + kReduceCols - 1) / kReduceCols : 1 << 20; }
+
 __global__ __launch_bounds__(1024) void reduce_partials_kernel(const float* __restrict__ partial, int P, int d, float* __restrict__ dw,
                                                                float* __restrict__ db) {
-  constexpr int kCols = 32, kShares = 32, kBatch = 8;
+  constexpr int kCols = kReduceCols, kShares = 32, kBatch = 8;
   __shared__ float sum[kShares][kCols + 1];
-  const int lane = threadIdx.x % kCols, share = threadIdx.x / kCols, col = blockIdx.x * kCols + lane;
+  const int lane = threadIdx.x % kCols, share = threadIdx.x / kCols;
   float* out = blockIdx.y ? db : dw;
   if (!out) return;
-  const float* p = partial + static_cast<int64_t>(blockIdx.y) * P * d + (col < d ? col : d - 1);
-  float s = 0.f;
-  for (int i = share; i < P; i += kShares * kBatch) {
-    float v[kBatch];
+  for (int64_t col0 = static_cast<int64_t>(blockIdx.x) * kCols; col0 < d; col0 += static_cast<int64_t>(gridDim.x) * kCols) {
+    const int64_t col = col0 + lane;
+    const float* p = partial + static_cast<int64_t>(blockIdx.y) * P * d + (col < d ? col : d - 1);
+    float s = 0.f;
+    for (int i = share; i < P; i += kShares * kBatch) {
+      float v[kBatch];
 #pragma unroll
-    for (int k = 0; k < kBatch; ++k) v[k] = i + k * kShares < P ? p[static_cast<int64_t>(i + k * kShares) * d] : 0.f;
+      for (int k = 0; k < kBatch; ++k) v[k] = i + k * kShares < P ? p[static_cast<int64_t>(i + k * kShares) * d] : 0.f;
 #pragma unroll
-    for (int k = 0; k < kBatch; ++k) s += v[k];
-  }
-  sum[share][lane] = s;
-  __syncthreads();
-  if (share == 0 && col < d) {
-    s = 0.f;
+      for (int k = 0; k < kBatch; ++k) s += v[k];
+    }
+    sum[share][lane] = s;
+    __syncthreads();
+    if (share == 0 && col < d) {
+      s = 0.f;
 #pragma unroll
-    for (int i = 0; i < kShares; ++i) s += sum[i][lane];
-    out[col] = s;
+      for (int i = 0; i < kShares; ++i) s += sum[i][lane];
+      out[col] = s;
+    }
+    __syncthreads();                     // the next columns' sums take these ones' place
   }
 }
 

@@ -193,7 +193,7 @@ int sdden_layernorm_backward(int32_t R, int32_t d, const void* dy, int32_t dy_ty
     by_type(vec, x_type, dy_type, [&](auto v, auto tx, auto ty) { norm_backward<decltype(v)::value, decltype(tx), decltype(ty)>(a, P, st); });
   }
   if (grads)
-    hipLaunchKernelGGL(lnorm::reduce_partials_kernel, dim3((d + 31) / 32, 2), dim3(1024), 0, st, a.partial, P, d, dweight, dbias);
+    hipLaunchKernelGGL(lnorm::reduce_partials_kernel, dim3(lnorm::reduce_grid(d), 2), dim3(1024), 0, st, a.partial, P, d, dweight, dbias);
   return done(what, hipGetLastError());
 }
 
