@@ -155,7 +155,8 @@ int sdden_layernorm_forward(int32_t R, int32_t d, const void* x, int32_t x_type,
   if (R < 0 || d <= 0 || !type_ok(x_type) || !type_ok(y_type) || x_stride < d || y_stride < d || (R > 0 && (!x || !y)) || !mean != !rstd)
     return sdi::fail(LAYER_ERR, SD_ERR_ARG, "%s: bad argument", what);
   if (!(eps >= 0.f) || std::isinf(eps)) return sdi::fail(LAYER_ERR, SD_ERR_ARG, "%s: eps must be finite and not negative", what);
-  if (!aligned_to(x, size_of(x_type)) || !aligned_to(y, size_of(y_type)) || !aligned_to(weight, 4) || !aligned_to(bias, 4))
+  if (!aligned_to(x, size_of(x_type)) || !aligned_to(y, size_of(y_type)) || !aligned_to(weight, 4) || !aligned_to(bias, 4) ||
+      !aligned_to(mean, 4) || !aligned_to(rstd, 4))
     return sdi::fail(LAYER_ERR, SD_ERR_ARG, "%s: a pointer is not aligned to its element type", what);
   if (R > kMaxRows || d > kMaxWidth) return sdi::fail(LAYER_ERR, SD_ERR_UNSUPPORTED, "%s: R=%d and d=%d must not exceed 2^30", what, R, d);
   if (R == 0) return SD_OK;
@@ -175,7 +176,8 @@ int sdden_layernorm_backward(int32_t R, int32_t d, const void* dy, int32_t dy_ty
       (R > 0 && (!x || !dy || !dx || !mean || !rstd)))
     return sdi::fail(LAYER_ERR, SD_ERR_ARG, "%s: bad argument", what);
   if (!aligned_to(x, size_of(x_type)) || !aligned_to(dx, size_of(x_type)) || !aligned_to(dres, size_of(x_type)) ||
-      !aligned_to(dy, size_of(dy_type)) || !aligned_to(weight, 4) || !aligned_to(workspace, 4))
+      !aligned_to(dy, size_of(dy_type)) || !aligned_to(weight, 4) || !aligned_to(mean, 4) || !aligned_to(rstd, 4) ||
+      !aligned_to(dweight, 4) || !aligned_to(dbias, 4) || !aligned_to(workspace, 4))
     return sdi::fail(LAYER_ERR, SD_ERR_ARG, "%s: a pointer is not aligned to its element type", what);
   if (R > kMaxRows || d > kMaxWidth) return sdi::fail(LAYER_ERR, SD_ERR_UNSUPPORTED, "%s: R=%d and d=%d must not exceed 2^30", what, R, d);
   const bool grads = dweight || dbias;
