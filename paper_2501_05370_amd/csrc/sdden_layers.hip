@@ -34,7 +34,7 @@ Width width_of(int d) { return d <= 1024 ? kWave : d <= 4096 ? k256 : d <= 12288
 // second for adding the partial rows up), 512 147 + 5.
 int partial_rows(int R, int d) {
   if (d > 16384) return std::min(R, 64);
-  if (d <= 1024) return std::min((R + 3) / 4, 1024);
+  if (d <= 1024) return std::min(R / 4 + (R % 4 != 0), 1024);
   return std::min(R, d <= 4096 ? 1024 : 512);
 }
 
