@@ -56,7 +56,7 @@ int sdden_mlp_create(int32_t d, int32_t H, int32_t E, const uint16_t* W1, const 
  * 32, 64 or a multiple of 128): scale = bf16(max |w| / 7), q = round(w / scale) + 8, quantised here from the bf16 weights; the
  * time embedding and the biases stay as they are.  Rows and activations are bf16 as in sdden_mlp_create.  Any d and H up to 2^20.
  * 4.1 to 4.5 bits per weight on the device.  Meant for the draft side of the independent drafter: a quarter of the target's bytes.
- * A prediction does not depend on the call it is part of. */
+ * A prediction does not depend on the call it is part of.  Weights to be quantised that are not finite are refused (SD_ERR_ARG). */
 int sdden_mlp4_create(int32_t d, int32_t H, int32_t E, int32_t group, const uint16_t* W1, const float* b1, const uint16_t* W2,
                       const float* b2, const uint16_t* W3, const float* b3, int32_t T, int32_t Rmax, sdden** out);
 

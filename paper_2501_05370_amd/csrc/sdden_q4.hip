@@ -86,8 +86,14 @@ float bf16_round(float x) {          // to nearest even; finite values only
   return x;
 }
 
-// W [K, N] bf16 (row = input) -> q [N, ceil(K/2)], scale [N, ceil(K/group)]: scale = bf16(max |w| / 7) over the group's inputs,
-// q = round(w / scale) + 8 within 0..15; a group of zeros has scale 0 and q = 8.
+bool all_finite(const uint16_t* W, size_t n) {
+  bool ok = true;
+  for (size_t i = 0; i < n; ++i) ok &= (W[i] & 0x7F80u) != 0x7F80u;
+  return ok;
+}
+
+// W [K, N] bf16, finite (row = input) -> q [N, ceil(K/2)], scale [N, ceil(K/group)]: scale = bf16(max |w| / 7) over the group's
+// inputs, q = round(w / scale) + 8 within 0..15; a group of zeros has scale 0 and q = 8.
 void quantize(const uint16_t* W, int K, int N, int group, std::vector<uint8_t>& q, std::vector<uint16_t>& scale) {
   const int groups = q4::groups_of(K, group);
   const size_t rowbytes = (static_cast<size_t>(K) + 1) / 2;
@@ -228,6 +234,11 @@ extern "C" int sdden_mlp4_create(int32_t d, int32_t H, int32_t E, int32_t group,
   if ((group != 32 && group != 64 && (group <= 0 || group % 128)) || d > q4::kMaxDim || H > q4::kMaxDim)
     return sdi::fail(Q4_ERR, SD_ERR_UNSUPPORTED, "%s: group=%d must be 32, 64 or a multiple of 128, d=%d and H=%d at most %d", what, group, d, H,
                      q4::kMaxDim);
+  // 4 bits have no infinity and no NaN to stand for one: a broken network would become a plausible one
+  const struct { const uint16_t* W; size_t n; const char* name; } matrices[] = {
+      {W1, static_cast<size_t>(d) * H, "W1"}, {W2, static_cast<size_t>(H) * H, "W2"}, {W3, static_cast<size_t>(H) * d, "W3"}};
+  for (const auto& w : matrices)
+    if (!all_finite(w.W, w.n)) return sdi::fail(Q4_ERR, SD_ERR_ARG, "%s: %s has weights that are not finite", what, w.name);
   std::unique_ptr<Mlp4Denoiser> m(new Mlp4Denoiser);
   m->d = d; m->T = T; m->H = H;
   const std::vector<float> tb = sdtime::table(T, H, E, b1, W1 + static_cast<size_t>(d) * H);
