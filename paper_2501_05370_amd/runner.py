@@ -3,8 +3,6 @@ from __future__ import annotations
 
 import torch
 
-from workloads import GatedParams, Q4MLPParams
-
 from .binding import Context, Denoiser
 from .sampler import DiffusionSampler, EfficientFrozenSampler, IndependentDrafterSampler, LangevinSampler, Phi4LangevinSampler
 
@@ -17,12 +15,13 @@ def make_context(cfg, seed=None) -> Context:
 
 
 def make_denoiser(cfg, max_rows: int, params=None) -> Denoiser:
-    """The denoiser of ``cfg``'s parameters, or of ``params``: of the workload's kind, or one of the networks that have a type of
-    their own (4-bit and gated ones), which serve as target or draft of any diffusion workload."""
+    """The denoiser of ``cfg``'s parameters, or of ``params``: of the workload's kind, or one of the networks that serve as target
+    or draft of any diffusion workload, which are known by their fields: ``p`` and ``group`` (a network to be kept in 4 bits) or
+    ``norm_weight`` (gated blocks)."""
     p, s = (cfg.params if params is None else params), cfg.schedule
-    if isinstance(p, Q4MLPParams):
+    if hasattr(p, "p") and hasattr(p, "group"):
         return Denoiser.sdden_mlp4_create(p.p, p.group, cfg.T, max_rows)
-    if isinstance(p, GatedParams):
+    if hasattr(p, "norm_weight"):
         return Denoiser.sdden_gated_create(p, cfg.T, max_rows)
     if cfg.kind == "gmm":
         return Denoiser.sdden_gmm_create(p.means, p.stds, p.logw, s.alpha_bar_state)
