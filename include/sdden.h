@@ -193,9 +193,11 @@ int sdden_gated_backward(int32_t R, int32_t d, int32_t H, int32_t act, const uin
  * scale [N, ceil(K/group)] bf16 bit patterns: host, read during the call, which lays the matrix out on the current device in the
  * kernels' order and waits for that.  group: 32, 64 or a multiple of 128 (K: one scale per row); N, K <= 2^20, any size.
  * sdden_q4_eval: X [R,K] and Y [R,N] of SDDEN_F32 or SDDEN_BF16 with any stride, bias [N] fp32 or NULL: dev, on the matrix's
- * device.  bf16 and fp32 rows enter exactly (an fp32 value as the sum of three bf16 ones: |x| < 2^127), sums are fp32, the output is
- * rounded once.  Sums are taken in one order for every R: a row's result does not depend on the call it is part of.  A row
- * with an infinity or a NaN gives NaN.  The handle is read only: any number of calls may use it at once, on any streams of its
+ * device.  bf16 and fp32 rows enter exactly, an fp32 value as the sum of three bf16 ones (from |x| = 2^-103 on; of smaller values what
+ * lies below 2^-126 may be lost).  Sums are fp32, the output is rounded once.  The sum of a group of inputs (a block of 128 of a
+ * larger group) starts from -8 sum(x) and is scaled when it is complete, so 24 sum |x| over it has to stay below 2^128: it does
+ * where |x| < 2^116; beyond that a result may be infinite or NaN although its value is not.  A row with an infinity or a NaN
+ * gives NaN.  Sums are taken in one order for every R: a row's result does not depend on the call it is part of.  The handle is read only: any number of calls may use it at once, on any streams of its
  * device, also captured ones, as long as it lives.  Errors: text in sdden_last_error(NULL). */
 typedef struct sdden_q4 sdden_q4;
 int sdden_q4_create(int32_t N, int32_t K, int32_t group, const uint8_t* q, const uint16_t* scale, sdden_q4** out);

@@ -9,7 +9,9 @@
 //   the -8      the sum of a group starts from -8 sum(x), which matrix instructions with a constant operand leave in just the
 //               layout of the sum; one such chain serves all the columns a wavefront computes on the same rows.  (Summed by the
 //               vector units as the rows are written to LDS, 512 rows x 4096 x 12288 take 92 us instead of 81: those bound the call.)
-//   fp32 rows   are three bf16 pieces (8 + 8 + 8 bits: exact) that take three rows of the tile; the epilogue adds them up
+//   fp32 rows   are three bf16 pieces (8 + 8 + 8 bits: exact while the last bit is a normal bf16 number, |x| >= 2^-103) that take
+//               three rows of the tile; the epilogue adds them up
+//   range       a group's sum holds up to 8 |x| from its start and 15 |x| from the products, unscaled: 24 sum |x| < 2^128
 // The order of a sum is the same everywhere: within a group along k, the groups of the blocks b = i, i + 8, i + 16, ... (128 k
 // each) in that order for i = 0 .. 7, and then those eight sums; so a row's result does not depend on the call it is part of.
 //

@@ -1,4 +1,4 @@
-"""4-bit matrices at the ends of what a call takes: the largest groups, more rows than one launch holds."""
+"""4-bit matrices at the ends of what a call takes: the largest groups, more rows than one launch holds, the largest and smallest values."""
 import numpy as np
 import pytest
 import torch
@@ -43,4 +43,33 @@ def test_more_rows_than_a_launch_holds(K, N, tx, R):
     whole = R // period * period
     assert torch.equal(y[:whole].view(-1, period, N), want.expand(whole // period, period, N))
     assert torch.equal(y[whole:R], want[:R - whole]) and y[R].isnan().all()
+    m.close()
+
+
+def test_the_range_of_the_rows():
+    """Rows of values just below 2^116 with the signs and levels that make a group's unscaled sum largest, single values where 24 |x| is
+    just below 2^128, and small fp32 values of 24 bits down to 2^-103.  Roundings as in the products' own test: 8 of a block's
+    instructions, one scaled add, 26 of shares, pieces and bias, each 2^-23 of sum (q + 8) |x| s at most."""
+    K, N = 128, 32
+    rng = np.random.default_rng(4)
+    q = rng.integers(0, 16, size=(N, K), dtype=np.uint8)
+    q[0], q[1], q[2] = 15, 0, 8
+    s = torch.full((N, 1), 2.0 ** -9, dtype=BF)
+    m = B.Q4Matrix.sdden_q4_create(q[:, 0::2] | (q[:, 1::2] << 4), s.view(torch.int16).numpy(), K, 128)
+    level = torch.from_numpy(q.astype(np.float64))
+    full = 1 + torch.from_numpy(rng.integers(0, 1 << 23, size=K) | 1).double() * 2.0 ** -23      # 24 bits, the last one set
+    rows = [torch.full((K,), 2.0 ** 116 * (1 - 2.0 ** -8)), -torch.full((K,), 2.0 ** 116 * (1 - 2.0 ** -8)), full * 2.0 ** 114,
+            full * 2.0 ** -102, full * 2.0 ** -103]
+    one = torch.zeros(K, dtype=torch.float64)
+    one[77] = 2.0 ** 123 * 1.25
+    rows += [one, -one]
+    x = torch.stack([r.double() for r in rows])
+    for R in (len(rows), 5, 40, 130):
+        for t in (F32, BF):
+            xt = x.repeat(-(-R // len(rows)), 1)[:R].to(t).cuda()
+            y = torch.empty(R, N, device="cuda")
+            m.sdden_q4_eval(xt, y)
+            xd = xt.double().cpu()
+            want, terms = xd @ (level - 8).T * 2.0 ** -9, xd.abs() @ (level + 8).T * 2.0 ** -9
+            assert bool(((y.double().cpu() - want).abs() <= 35 * 2.0 ** -23 * terms).all()), (R, t)
     m.close()
