@@ -43,6 +43,8 @@ inline int fail(std::string& slot, int code, const char* fmt, ...) {
   vsnprintf(buf, sizeof buf, fmt, ap);
   va_end(ap);
   slot = buf;
+  // the caller has it now: the runtime would hand it to whoever asks for the last launch's error next, the caller's own calls included
+  if (code == SD_ERR_HIP) (void)hipGetLastError();
   return code;
 }
 
