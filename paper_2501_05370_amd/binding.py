@@ -525,6 +525,13 @@ def _flat(t: Optional[torch.Tensor], name: str, shape, dtype, allow_none: bool =
                   f"{tuple(t.shape)} on {t.device}, contiguous={t.is_contiguous()}")
 
 
+def _hidden_width(Wg) -> int:
+    """H of the gate weights [H,d], from which the other shapes follow."""
+    if Wg is None or len(Wg.shape) != 2:
+        raise SDError(f"Wg: need a matrix [H,d], got {None if Wg is None else tuple(Wg.shape)}")
+    return Wg.shape[0]
+
+
 def _scratch(t: Optional[torch.Tensor], name: str):
     """(pointer, bytes) of a caller's workspace, any contiguous tensor."""
     if t is None:
@@ -588,7 +595,7 @@ def sdden_gated_forward(X, Wg, Wu, Wd, Y, hidden, gates=None, act: int = SDDEN_S
     bf = _BF16
     xp, xs = _rows(X, "X", only=bf)
     R, d = X.shape
-    H = Wg.shape[0]
+    H = _hidden_width(Wg)
     yp, ys = _rows(Y, "Y", (R, d))
     rp, rs = _rows(res, "res", (R, d), Y.dtype, True)
     if res is not None and R > 1 and rs != ys:
@@ -606,7 +613,7 @@ def sdden_gated_backward(dY, X, Wg, Wu, Wd, gates, hidden, dX, dWg, dWu, dWd, wo
     bf = _BF16
     xp, xs = _rows(X, "X", only=bf)
     R, d = X.shape
-    H = Wg.shape[0]
+    H = _hidden_width(Wg)
     dyp, dys = _rows(dY, "dY", (R, d), bf)
     dxp, dxs = _rows(dX, "dX", (R, d), bf, True)
     tw = torch.float32 if dWg is None else dWg.dtype

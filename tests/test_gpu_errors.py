@@ -26,3 +26,18 @@ def test_calls_after_one_that_ran_out_of_memory(what):
     x64 = x.double()
     want = (x64 - x64.mean(1, keepdim=True)) / (x64.var(1, unbiased=False, keepdim=True) + 1e-5).sqrt()
     assert bool(((y.double() - want).abs() <= 1e-5 * want.abs().max()).all())
+
+
+def test_the_gated_block_without_a_tensor_it_needs():
+    """A missing tensor, or one of another shape, is named."""
+    x, w, wd = torch.randn(4, 64, device="cuda").bfloat16(), torch.randn(16, 64, device="cuda").bfloat16(), torch.randn(64, 16, device="cuda").bfloat16()
+    y, hidden, gates = torch.empty_like(x), torch.empty(4, 16, dtype=torch.bfloat16, device="cuda"), torch.empty(2, 4, 16, device="cuda")
+    for name, args in (("Wg", (x, None, w, wd, y, hidden)), ("Wg", (x, w[0, 0], w, wd, y, hidden)), ("Wg", (x, w[0], w, wd, y, hidden)),
+                       ("Wu", (x, w, None, wd, y, hidden)), ("Wd", (x, w, w, None, y, hidden)), ("Y", (x, w, w, wd, None, hidden)),
+                       ("hidden", (x, w, w, wd, y, None)), ("X", (None, w, w, wd, y, hidden))):
+        with pytest.raises(B.SDError, match=f"{name}:"):
+            B.sdden_gated_forward(*args)
+    ws = torch.empty(B.sdden_gated_workspace_bytes(4, 64, 16), dtype=torch.uint8, device="cuda")
+    for name, args in (("Wg", (y, x, None, w, wd, gates, hidden)), ("dY", (None, x, w, w, wd, gates, hidden)), ("gates", (y, x, w, w, wd, None, hidden))):
+        with pytest.raises(B.SDError, match=f"{name}:"):
+            B.sdden_gated_backward(*args, torch.empty_like(x), None, None, None, ws)
