@@ -72,16 +72,28 @@ static __device__ const u32x4 g_zeros = {0, 0, 0, 0};
 __device__ __forceinline__ float sigmoid(float x) { return __frcp_rn(1.0f + __expf(-x)); }
 
 // f(g) and, for the backward pass, f'(g).  SiLU: g s, s + g s (1 - s).  GELU: g P, P + g p with the normal distribution's
-// integral P (the library's erff) and density p.
+// integral P and density p.  P's tail is e^(-g^2 / 2) t A(t), t = 1 / (1 + 0.27 |g|): all its digits wherever the exponential has
+// them, where (1 + erf(g / sqrt 2)) / 2 has none left below g = -5, and the exponential is p's.  A: least squares in the relative error,
+// reweighted towards the smallest largest one, over |g| <= 14.5 where the tail leaves fp32; 2.4e-8 off at most, 4e-7 evaluated in fp32.
 __device__ __forceinline__ void activation(int act, float g, float& f, float& df) {
   if (act == kSilu) {
     const float s = sigmoid(g);
     f = g * s;
     df = s + f * (1.0f - s);
   } else {
-    const float P = 0.5f * (1.0f + erff(g * 0.70710678118654752f));
+    const float t = __builtin_amdgcn_rcpf(__builtin_fmaf(0.27f, __builtin_fabsf(g), 1.0f)), e = __expf(-0.5f * g * g);
+    float a = 0.028961092233657837f;
+    a = __builtin_fmaf(a, t, -0.12648582458496094f);
+    a = __builtin_fmaf(a, t, 0.16978608071804047f);
+    a = __builtin_fmaf(a, t, -0.06921068578958511f);
+    a = __builtin_fmaf(a, t, 0.10782558470964432f);
+    a = __builtin_fmaf(a, t, 0.07204962521791458f);
+    a = __builtin_fmaf(a, t, 0.10181060433387756f);
+    a = __builtin_fmaf(a, t, 0.10754287242889404f);
+    a = __builtin_fmaf(a, t, 0.10772065818309784f);
+    const float tail = e * (t * a), P = g < 0.0f ? tail : 1.0f - tail;
     f = g * P;
-    df = P + g * 0.39894228040143268f * __expf(-0.5f * g * g);
+    df = P + g * 0.39894228040143268f * e;
   }
 }
 
