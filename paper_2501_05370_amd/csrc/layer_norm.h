@@ -4,8 +4,10 @@
 //   g = dy w:  dx = r (g - mean(g) - xh mean(g xh)) [+ dres],   dw = sum over rows dy xh,   db = sum over rows dy
 //
 // Bound by HBM: each row is read once and kept in registers (E elements per thread of the TPR threads that share a row), so the
-// variance is the two-pass one, the sum of (x - mean)^2 around the finished mean, at no further traffic; everything between the
-// loads and the stores is fp32.  Rows longer than the widest register form are walked in three passes, out of L2.
+// variance is the two-pass one, the sum of (x - m)^2 around the finished mean m, at no further traffic; everything between the
+// loads and the stores is fp32.  m carries the roundings of a sum as large as the row's offset, so the sum of (x - m), taken with
+// that of the squares, gives what it is off by (without it, rows at 1000 times their deviation had more than 1e-5 of it in every
+// y).  Rows longer than the widest register form are walked in three passes, out of L2.
 // Measured: 7680 fp32 rows of 12288 to bf16 121 us (4.7 TB/s; a large copy reaches 4.8), 16384 bf16 rows of 4096 forward 55 us
 // (4.8 TB/s), backward with dres 101 us (5.3 TB/s, part of x still cached) and 7 us for the weights' gradients; one row 4 us.
 // The weights' gradients need a sum over all rows: a workgroup walks rows blockIdx, blockIdx + grid, ... with its columns'
@@ -72,7 +74,20 @@ __device__ __forceinline__ void store(T* p, const float (&v)[V]) {
 
 using sdlane::wave_sum;
 
-// Sums of a and b over the TPR threads of a row; `slot` alternates between calls so that one barrier per call is enough.
+// Sum of a, or sums of a and b, over the TPR threads of a row; `slot` alternates between calls so that one barrier per call is enough.
+template <int TPR>
+__device__ __forceinline__ void row_sum(float& a, float2 (&red)[2][16], int slot) {
+  a = wave_sum(a);
+  if constexpr (TPR > 64) {
+    constexpr int NW = TPR / 64;
+    if ((threadIdx.x & 63) == 0) red[slot][threadIdx.x >> 6].x = a;
+    __syncthreads();
+    a = 0.f;
+#pragma unroll
+    for (int w = 0; w < NW; ++w) a += red[slot][w].x;
+  }
+}
+
 template <int TPR>
 __device__ __forceinline__ void row_sum2(float& a, float& b, float2 (&red)[2][16], int slot) {
   a = wave_sum(a);
@@ -88,6 +103,12 @@ __device__ __forceinline__ void row_sum2(float& a, float& b, float2 (&red)[2][16
       b += red[slot][w].y;
     }
   }
+}
+
+// From the mean square around a value that the mean is `off` from.  (A NaN stays one.)
+__device__ __forceinline__ float rstd_of(float square, float off, float eps) {
+  const float var = square - off * off;
+  return 1.0f / sqrtf((var < 0.f ? 0.f : var) + eps);
 }
 
 constexpr int threads_of(int tpr) { return tpr < 256 ? 256 : tpr; }
@@ -122,7 +143,7 @@ __global__ __launch_bounds__(threads_of(TPR)) void forward_kernel(Args p) {
   if (r < p.R) fetch(r);
   for (; r < p.R; r += static_cast<int64_t>(gridDim.x) * RPB) {
     float v[C][V];
-    float s = 0.f, unused = 0.f;
+    float s = 0.f;
 #pragma unroll
     for (int c = 0; c < C; ++c)
       if ((c * TPR + t) * V < p.d) {
@@ -134,32 +155,33 @@ __global__ __launch_bounds__(threads_of(TPR)) void forward_kernel(Args p) {
       }
     const int64_t next = r + static_cast<int64_t>(gridDim.x) * RPB;
     if (next < p.R) fetch(next);
-    row_sum2<TPR>(s, unused, red, 0);
-    const float mean = s * inv_d;
-    float q = 0.f;
-    unused = 0.f;
+    row_sum<TPR>(s, red, 0);
+    const float about = s * inv_d;
+    float q = 0.f, rest = 0.f;
 #pragma unroll
     for (int c = 0; c < C; ++c)
       if ((c * TPR + t) * V < p.d) {
 #pragma unroll
         for (int e = 0; e < V; ++e) {
-          v[c][e] -= mean;
+          v[c][e] -= about;
           q += v[c][e] * v[c][e];
+          rest += v[c][e];
         }
       }
-    row_sum2<TPR>(q, unused, red, 1);
-    const float rstd = 1.0f / sqrtf(q * inv_d + p.eps);
+    row_sum2<TPR>(q, rest, red, 1);
+    const float off = rest * inv_d, rstd = rstd_of(q * inv_d, off, p.eps);
     if (t == 0 && p.mean) {
-      p.mean[r] = mean;
+      p.mean[r] = about + off;
       p.rstd[r] = rstd;
     }
     TY* y = static_cast<TY*>(p.y) + r * p.ldy;
+    const float shift = -off * rstd;
 #pragma unroll
     for (int c = 0; c < C; ++c) {
       const int col = (c * TPR + t) * V;
       if (col < p.d) {
 #pragma unroll
-        for (int e = 0; e < V; ++e) v[c][e] = v[c][e] * rstd * w[c][e] + b[c][e];
+        for (int e = 0; e < V; ++e) v[c][e] = __builtin_fmaf(__builtin_fmaf(v[c][e], rstd, shift), w[c][e], b[c][e]);
         store<V, KEEP>(y + col, v[c]);
       }
     }
@@ -174,24 +196,25 @@ __global__ __launch_bounds__(1024) void forward_long_kernel(Args p) {
   for (int64_t r = blockIdx.x; r < p.R; r += gridDim.x) {
     const TX* x = static_cast<const TX*>(p.x) + r * p.ldx;
     TY* y = static_cast<TY*>(p.y) + r * p.ldy;
-    float s = 0.f, q = 0.f, unused = 0.f;
+    float s = 0.f, q = 0.f;
     for (int c = threadIdx.x; c < p.d; c += 1024) s += static_cast<float>(x[c]);
-    row_sum2<1024>(s, unused, red, 0);
-    const float mean = s / static_cast<float>(p.d);
+    row_sum<1024>(s, red, 0);
+    const float about = s / static_cast<float>(p.d);
+    float rest = 0.f;
     for (int c = threadIdx.x; c < p.d; c += 1024) {
-      const float v = static_cast<float>(x[c]) - mean;
+      const float v = static_cast<float>(x[c]) - about;
       q += v * v;
+      rest += v;
     }
-    unused = 0.f;
-    row_sum2<1024>(q, unused, red, 1);
-    const float rstd = 1.0f / sqrtf(q / static_cast<float>(p.d) + p.eps);
+    row_sum2<1024>(q, rest, red, 1);
+    const float off = rest / static_cast<float>(p.d), rstd = rstd_of(q / static_cast<float>(p.d), off, p.eps);
     if (threadIdx.x == 0 && p.mean) {
-      p.mean[r] = mean;
+      p.mean[r] = about + off;
       p.rstd[r] = rstd;
     }
     for (int c = threadIdx.x; c < p.d; c += 1024) {
       const float w = p.w ? p.w[c] : 1.f, b = p.b ? p.b[c] : 0.f;
-      y[c] = static_cast<TY>((static_cast<float>(x[c]) - mean) * rstd * w + b);
+      y[c] = static_cast<TY>((static_cast<float>(x[c]) - about - off) * rstd * w + b);
     }
   }
 }
