@@ -55,7 +55,8 @@ int sdden_mlp_create(int32_t d, int32_t H, int32_t E, const uint16_t* W1, const 
 /* The same network with W1's first d rows, W2 and W3 kept in 4 bits with one bf16 scale per `group` inputs of an output (group:
  * 32, 64 or a multiple of 128): scale = bf16(max |w| / 7), q = round(w / scale) + 8, quantised here from the bf16 weights; the
  * time embedding and the biases stay as they are.  Rows and activations are bf16 as in sdden_mlp_create.  Any d and H up to 2^20.
- * 4.1 to 4.5 bits per weight on the device.  Meant for the draft side of the independent drafter: a quarter of the target's bytes.
+ * 4.1 to 4.5 bits per weight on the device.  Meant for the draft side of the independent drafter with few chains: a quarter of the
+ * target's bytes, which is what calls of up to about 32 rows wait for; from 64 rows on the bf16 network is as fast or faster.
  * A prediction does not depend on the call it is part of.  Weights to be quantised that are not finite are refused (SD_ERR_ARG). */
 int sdden_mlp4_create(int32_t d, int32_t H, int32_t E, int32_t group, const uint16_t* W1, const float* b1, const uint16_t* W2,
                       const float* b2, const uint16_t* W3, const float* b3, int32_t T, int32_t Rmax, sdden** out);
@@ -130,6 +131,7 @@ int sdden_profile_collect(sdden* den, double* total_ms, int64_t* launches);
 int sdden_mlp_select_gemm(sdden* den, int32_t variant);
 
 int sdden_destroy(sdden* den);
+/* Text of the last error of `den`, or with NULL of this thread's last call that had no denoiser (creates, layers, 4-bit matrices). */
 const char* sdden_last_error(const sdden* den);
 
 /* ---- Layers of row networks ------------------------------------------------------------------------------------------
@@ -146,7 +148,8 @@ const char* sdden_last_error(const sdden* den);
 
 /* Layer norm:  y = (x - mean) rstd * weight + bias,  rstd = 1 / sqrt(mean((x - mean)^2) + eps), statistics in fp32.
  * x [R,d] of x_type, y [R,d] of y_type (any mix), weight and bias [d] fp32 or NULL (1 and 0), mean and rstd [R] fp32: both
- * written for the backward pass, or both NULL.  Any d from 1 to 2^30, any stride >= d, any alignment of the element type; 16-byte
+ * written for the backward pass, or both NULL.  y keeps its digits in rows far from zero; the backward pass takes the mean as fp32 holds
+ * it, so x - mean is off there by up to 2^-25 |mean|.  Any d from 1 to 2^30, any stride >= d, any alignment of the element type; 16-byte
  * accesses are used where d, the strides and the pointers allow them. */
 int sdden_layernorm_forward(int32_t R, int32_t d, const void* x, int32_t x_type, int64_t x_stride, const float* weight,
                             const float* bias, float eps, void* y, int32_t y_type, int64_t y_stride, float* mean, float* rstd,

@@ -8,8 +8,8 @@
 // loads and the stores is fp32.  m carries the roundings of a sum as large as the row's offset, so the sum of (x - m), taken with
 // that of the squares, gives what it is off by (without it, rows at 1000 times their deviation had more than 1e-5 of it in every
 // y).  Rows longer than the widest register form are walked in three passes, out of L2.
-// Measured: 7680 fp32 rows of 12288 to bf16 121 us (4.7 TB/s; a large copy reaches 4.8), 16384 bf16 rows of 4096 forward 55 us
-// (4.8 TB/s), backward with dres 101 us (5.3 TB/s, part of x still cached) and 7 us for the weights' gradients; one row 4 us.
+// Measured: 7680 fp32 rows of 12288 to bf16 121 us (4.7 TB/s; a copy by rows reaches 5.4), 16384 bf16 rows of 4096 forward 54 us
+// (5.0 TB/s), backward with dres 99 us (5.4 TB/s, part of x still cached) and 7 us for the weights' gradients; one row 4 us.
 // The weights' gradients need a sum over all rows: a workgroup walks rows blockIdx, blockIdx + grid, ... with its columns'
 // sums in registers and leaves one partial row; reduce_partials_kernel adds those up in a fixed order (no atomics: the
 // same bits every time).

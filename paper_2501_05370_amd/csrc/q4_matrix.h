@@ -46,7 +46,9 @@ hipError_t launch_rows(const Args& a, int R, hipStream_t st) {
     // More than 32 tile rows: groups of 64 with either kernel.  A workgroup of few_kernel (16 columns, one to a CU) takes an eighth of
     // the blocks of 128 k per wavefront, 2.1 us each and 2.5 us around them; one of many_kernel (128 columns, two to a CU, one for groups of 32)
     // all of them at 1 us (1.5).  us measured (bf16 rows), few / many:  12288 x 4096, 64 rows 28 / 89, 128 rows 57 / 90, 192 rows 83 / 92;  4096 x 4096, 64 rows
-    // 13 / 38;  4096 x 12288, 64 rows 34 / 35, 128 rows 68 / 35.
+    // 13 / 38;  4096 x 12288, 64 rows 34 / 35, 128 rows 68 / 35.  fp32 rows (three tile rows each):  12288 x 4096, 21 rows 37 / 116, 42 rows
+    // 68 / 116, 64 rows 124 / 118;  4096 x 12288, 21 rows 40 / 43, 42 rows 77 / 45;  4096 x 4096, groups of 64, 42 rows 28 / 46, 64 rows 53 / 46,
+    // groups of 32, 64 rows 56 / 61, 128 rows 96 / 61;  the rule takes the shorter time in each.
     const int64_t row_groups = (R + 64 / P - 1) / (64 / P), few = row_groups * a.ntiles, many = row_groups * ((a.ntiles + 7) / 8);
     const double few_us = static_cast<double>((few + 255) / 256) * (2.1 * ((a.kblocks + kShares - 1) / kShares) + 2.5);
     const double many_us = GPB < 4 ? static_cast<double>((many + 511) / 512) * a.kblocks : 1.5 * static_cast<double>((many + 255) / 256) * a.kblocks;

@@ -16,7 +16,8 @@
 // each) in that order for i = 0 .. 7, and then those eight sums; so a row's result does not depend on the call it is part of.
 //
 // Measured, us (matrices rotating through 75 MB, so from the memory-side cache at best): 12288 x 4096 (26 MB) one bf16 row 8.3, one
-// fp32 row 10.9, 64 bf16 rows 28; 4096 x 12288 19 rows 17, 512 rows 81 (0.63 PFLOP/s of products, and half as many again for the -8).
+// fp32 row 10.9, 64 bf16 rows 28; 4096 x 12288 19 rows 17, 512 rows 81 (0.63 PFLOP/s of products, and half as many again for the -8), 512 fp32
+// rows 267.  Registers: few_kernel<4, 1, 1, bf16, 16, 1> spills 44 bytes a lane, <2, 2, 1, rounded, 8, 2> 12, many_kernel<2, bf16> 20.
 //
 // Layout (made once, at create): 16 columns x 128 k are one block of 1 KiB, in which lane (l16, lq) finds its 16 bytes: dword
 // j holds column l16, k = 32 j + 8 lq .. + 7, elements 0..3 in the low halves of its bytes and 4..7 in the high ones.  The blocks
